@@ -339,6 +339,128 @@ int sscater_profile(sscater_t h, int32_t enable);
  * n >= 2L + 2 + n_ups entries; clears the record.  Synchronises `stream`. */
 int sscater_profile_read(sscater_t h, double* ms, int64_t* launches, int32_t n, void* stream);
 
+/* Token operators: what a program computes on the maps' cells ("tokens", rows
+ * of features) after a stride: linear layers, and attention over the tokens of
+ * the strides before, held in a cache.  They take no handle and keep nothing;
+ * the caller owns every buffer.  Their arguments are checked on the host
+ * (SSCATER_E_INVALID_ARG before anything is enqueued); they are asynchronous on
+ * `stream`, allocate nothing, can be captured into a graph, and run on the
+ * current device, which must be the stream's.  What only the device knows
+ * (lengths, positions) is kept inside the buffers by the kernels: contradictory
+ * values give undefined results, never an access outside. */
+
+typedef enum {
+    SSCATER_ACT_NONE = 0,
+    SSCATER_ACT_RELU = 1, /* max(z, 0); NaN stays NaN */
+    SSCATER_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2 */
+    SSCATER_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} sscater_activation;
+
+/* A linear layer over rows: y = act(x W^T + bias) + residual.
+ *   rows >= 0, cin, cout >= 1; x [rows][cin], W [cout][cin] (a 1x1 convolution's
+ *   OIHW weights), bias [cout], residual and y [rows][cout], all in dtype;
+ *   *_stride: elements between two rows, at least the row's length (ignored
+ *   for a null residual). */
+typedef struct {
+    int64_t rows;
+    int32_t cin, cout;
+    int32_t dtype;      /* sscater_dtype */
+    int32_t activation; /* sscater_activation */
+    int64_t x_stride, w_stride, residual_stride, y_stride;
+} sscater_linear_spec;
+
+/* bias and residual may be NULL.  y may be the residual itself (same pointer
+ * and stride) and must not overlap x, W or bias.  Sums are fp32; fp32 products
+ * are formed from three bf16 parts of either factor, which hold its 24 bits;
+ * bf16 outputs are rounded once.  A row may be aligned to its elements only;
+ * rows of x and W that are multiples of 16 bytes apart and start on one are
+ * read faster. */
+int sscater_linear(const sscater_linear_spec* spec, const void* x, const void* weight, const void* bias,
+                   const void* residual, void* y, void* stream);
+
+/* The keys and values of the tokens that later ones look back at, for `batch`
+ * independent streams of tokens.  k, v: device [batch][kv_heads][capacity]
+ * [head_dim] in dtype, on 16-byte boundaries; past: device int64[batch], the
+ * tokens a stream has seen.  Token j of a stream (j = 0 its first ever) sits in
+ * slot j if j < sinks, else in slot sinks + (j - sinks) mod (capacity - sinks):
+ * the first tokens stay, the others give way to the newest.
+ *   head_dim 32, 64 or 128; 0 <= sinks < capacity. */
+typedef struct {
+    int32_t dtype; /* sscater_dtype */
+    int32_t batch, kv_heads, head_dim;
+    int32_t sinks, capacity;
+    void* k;
+    void* v;
+    int64_t* past;
+} sscater_token_cache;
+
+/* The new tokens of a call: `tokens` rows, sequence b's being rows start[b] to
+ * start[b + 1] - 1 (start: device int32[batch + 1], increasing from 0 to
+ * tokens, or NULL: max_new rows each, tokens = batch * max_new).  max_new: the
+ * most that one sequence brings; max_past: no less than any past[b]. */
+typedef struct {
+    int32_t tokens, max_new;
+    int64_t max_past;
+    const int32_t* start;
+} sscater_token_rows;
+
+/* How sscater_tokens_append forms heads from projected rows.
+ *   qkv rows: q_heads query heads, kv_heads key heads, kv_heads value heads of
+ *   head_dim values each, qkv_stride elements from row to row;
+ *   axes (1..3), section[axes]: the head_dim / 2 pairs of a head are turned by
+ *   the first axis's position for section[0] pairs, then the second's, ...;
+ *   interleaved: pair i is values (2i, 2i + 1) instead of (i, i + head_dim / 2);
+ *   eps: of the norms. */
+typedef struct {
+    int32_t q_heads, axes;
+    int32_t section[3];
+    int32_t interleaved;
+    float eps;
+    int64_t qkv_stride;
+} sscater_head_spec;
+
+/* Query, key and value heads of the new tokens in one pass.  Each query and key
+ * head x becomes x / sqrt(mean(x^2) + eps) * weight (q_weight, k_weight: device
+ * [head_dim] in dtype; NULL: no norm), and its pair i is turned by
+ * pos[token][axis(i)] * inv_freq[i] radians (pos: device int32[tokens][axes],
+ * inv_freq: device float[head_dim / 2]; whole turns are taken off in 64 bits,
+ * so positions may be large).  Queries go to q, device [tokens][q_heads]
+ * [head_dim]; keys and values to the cache, at positions past[b] onwards (past
+ * itself is moved on by sscater_tokens_advance).  Of tokens that share a slot
+ * only the last is written. */
+int sscater_tokens_append(const sscater_head_spec* spec, const sscater_token_cache* cache,
+                          const sscater_token_rows* rows, const void* qkv, const void* q_weight, const void* k_weight,
+                          const float* inv_freq, const int32_t* pos, void* q, void* stream);
+
+/* Attention of the new tokens (already appended, past not yet moved on).
+ * Query head h of the token at position p of its stream reads key and value
+ * head h / (q_heads / kv_heads) of the positions j with
+ *   causal = 1: j <= p and (j > p - window or j < sinks);
+ *   causal = 0: every new token of the sequence, and those before with
+ *               j > past - window or j < sinks (a stride's tokens see one
+ *               another and the same past);
+ * out = sum_j softmax_j(scale * q . k_j) v_j, device [tokens][q_heads]
+ * [head_dim], as q; q and out on 16-byte boundaries.  window >= 1; q_heads a
+ * multiple of kv_heads.  The keys in reach must still be held: capacity - sinks
+ * at least min(window + max_new - 1, max_past + max_new), else
+ * SSCATER_E_INVALID_ARG. */
+typedef struct {
+    int32_t q_heads, window, causal;
+    float scale;
+} sscater_attend_spec;
+
+/* The workspace is device memory of sscater_tokens_workspace() bytes (0: none
+ * needed, workspace may be NULL), on a 16-byte boundary, free for reuse once
+ * the stream has executed the call; too small a one is SSCATER_E_INVALID_ARG. */
+int sscater_tokens_workspace(const sscater_attend_spec* spec, const sscater_token_cache* cache,
+                             const sscater_token_rows* rows, size_t* bytes);
+int sscater_tokens_attend(const sscater_attend_spec* spec, const sscater_token_cache* cache,
+                          const sscater_token_rows* rows, const void* q, void* out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* past[b] += the new tokens of sequence b. */
+int sscater_tokens_advance(const sscater_token_cache* cache, const sscater_token_rows* rows, void* stream);
+
 /* Static text for an error code; for SSCATER_E_HIP the last HIP error text of
  * the calling thread's most recent failing call. */
 const char* sscater_strerror(int code);

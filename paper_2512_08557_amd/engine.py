@@ -27,7 +27,8 @@ EXPORTS = ("sscater_create", "sscater_create_neck", "sscater_create_pfn", "sscat
            "sscater_create_batched", "sscater_step", "sscater_step_sorted",
            "sscater_step_points",
            "sscater_read", "sscater_reset", "sscater_destroy", "sscater_changed", "sscater_changed_noalloc",
-           "sscater_stats", "sscater_profile", "sscater_profile_read", "sscater_strerror")
+           "sscater_stats", "sscater_profile", "sscater_profile_read", "sscater_linear", "sscater_tokens_append",
+           "sscater_tokens_workspace", "sscater_tokens_attend", "sscater_tokens_advance", "sscater_strerror")
 
 
 class Grid(ctypes.Structure):
@@ -61,6 +62,33 @@ class Stats(ctypes.Structure):
                 ("pairs_total", ctypes.c_int64 * (MAX_LAYERS + 1)),
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double), ("n_ups", ctypes.c_int32),
                 ("up_pairs", ctypes.c_int64 * MAX_UPSAMPLERS)]
+
+
+class LinearSpec(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cin", ctypes.c_int32), ("cout", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("x_stride", ctypes.c_int64),
+                ("w_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
+
+
+class TokenCacheSpec(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("sinks", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("past", ctypes.c_void_p)]
+
+
+class TokenRows(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("max_new", ctypes.c_int32), ("max_past", ctypes.c_int64),
+                ("start", ctypes.c_void_p)]
+
+
+class HeadSpec(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("axes", ctypes.c_int32), ("section", ctypes.c_int32 * 3),
+                ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float), ("qkv_stride", ctypes.c_int64)]
+
+
+class AttendSpec(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("window", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 class SscaterError(RuntimeError):
@@ -103,6 +131,12 @@ def lib() -> ctypes.CDLL:
         L.sscater_profile.argtypes = [vp, i32]
         L.sscater_profile_read.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64), i32,
                                            vp]
+        cp, rp = ctypes.POINTER(TokenCacheSpec), ctypes.POINTER(TokenRows)
+        L.sscater_linear.argtypes = [ctypes.POINTER(LinearSpec), vp, vp, vp, vp, vp, vp]
+        L.sscater_tokens_append.argtypes = [ctypes.POINTER(HeadSpec), cp, rp, vp, vp, vp, vp, vp, vp, vp]
+        L.sscater_tokens_workspace.argtypes = [ctypes.POINTER(AttendSpec), cp, rp, ctypes.POINTER(ctypes.c_size_t)]
+        L.sscater_tokens_attend.argtypes = [ctypes.POINTER(AttendSpec), cp, rp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.sscater_tokens_advance.argtypes = [cp, rp, vp]
         L.sscater_strerror.argtypes = [ctypes.c_int]
         L.sscater_strerror.restype = ctypes.c_char_p
         for f in EXPORTS[:-1]:
