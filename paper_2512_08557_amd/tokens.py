@@ -13,60 +13,59 @@ from typing import Optional, Sequence
 import numpy as np
 
 from . import engine as E
-from .engine import BF16, F32, _check, lib
+from .engine import BF16, F32, SscaterError, _check, lib
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
 def _kind(t) -> int:
     import torch
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return F32
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return BF16
     raise ValueError(f"float32 or bfloat16 tensors, not {t.dtype}")
 
 
-def _require(t, name: str, like=None, dtype=None, shape=None):
-    """A cuda tensor of the given dtype (or like's dtype and device) and shape."""
+def _require(t, name: str, dtype, index: int, shape=None):
+    """A cuda tensor of the given dtype on device `index`, of the given shape."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a cuda tensor")
-    if like is not None and t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    want = dtype if dtype is not None else like.dtype if like is not None else t.dtype
-    if t.dtype != want:
-        raise ValueError(f"{name} must be {want}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, not on cuda:{index}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
     return t
 
 
-def _ptr(t):
-    return ctypes.c_void_p(t.data_ptr() if t is not None else None)
+def _dense(t, name: str, dtype, index: int, shape):
+    if not _require(t, name, dtype, index, shape).is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-class _On:
-    """The device of a call and its stream: a stream other than the current one
-    first waits for it, and the call's tensors are recorded there."""
-
-    def __init__(self, device, stream, tensors):
-        import torch
-        self._guard = torch.cuda.device(device)
-        self._torch, self._stream, self._tensors = torch, stream, tensors
-
-    def __enter__(self):
-        self._guard.__enter__()
-        cur = self._torch.cuda.current_stream()
-        s = self._stream if self._stream is not None else cur
-        if s != cur:
-            s.wait_stream(cur)
-            for t in self._tensors:
-                if t is not None:
-                    t.record_stream(s)
-        return ctypes.c_void_p(s.cuda_stream)
-
-    def __exit__(self, *exc):
-        return self._guard.__exit__(*exc)
+def _launch(fn, where: str, index: int, stream, tensors, *args) -> None:
+    """One library call on device `index`, on torch's current stream; another
+    stream first waits for that one, and the call's tensors are recorded there
+    (as in Engine).  The current stream's handle is asked for as a number: the
+    object around it costs more than the rest of the call."""
+    import torch
+    if stream is None and torch._C._cuda_getDevice() == index:
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            cur = torch.cuda.current_stream()
+            s = stream if stream is not None else cur
+            if s != cur:
+                s.wait_stream(cur)
+                for t in tensors:
+                    if t is not None:
+                        t.record_stream(s)
+            rc = fn(*args, s.cuda_stream)
+    if rc != E.OK:
+        raise SscaterError(rc, where)
 
 
 def _row_stride(t, name: str, width: int) -> int:
@@ -74,6 +73,8 @@ def _row_stride(t, name: str, width: int) -> int:
     run through one even stride."""
     if t.dim() < 1 or t.shape[-1] != width:
         raise ValueError(f"{name} must end in {width} values")
+    if t.is_contiguous():
+        return width
     if width > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the values of a row must be contiguous")
     if t.numel() == 0:
@@ -99,32 +100,33 @@ def linear(x, weight, bias=None, activation: Optional[str] = None, residual=None
     rows evenly apart), weight [cout, cin], bias [cout], residual and out
     [..., cout]; activation none, relu, gelu or silu.  out may be the residual
     and must not overlap the other operands."""
-    import torch
-    if activation not in ACTIVATIONS:
+    act = ACTIVATIONS.get(activation, -1)
+    if act < 0:
         raise ValueError(f"activation must be one of {sorted(k for k in ACTIVATIONS if k)}")
-    kind = _kind(x)
+    kind, dtype = _kind(x), x.dtype
     if weight.dim() != 2:
         raise ValueError("weight must be [cout, cin]")
     cout, cin = weight.shape
-    _require(x, "x")
-    _require(weight, "weight", like=x)
-    shape = tuple(x.shape[:-1]) + (cout,)
-    xs, ws = _row_stride(x, "x", cin), _row_stride(weight, "weight", cin)
+    if not x.is_cuda:
+        raise ValueError("x must be a cuda tensor")
+    index = x.get_device()
+    _require(weight, "weight", dtype, index)
+    xs, ws, rs = _row_stride(x, "x", cin), _row_stride(weight, "weight", cin), cout
+    shape = x.shape[:-1] + (cout,)
     if bias is not None:
-        _require(bias, "bias", like=x, shape=(cout,))
+        _require(bias, "bias", dtype, index, (cout,))
         if cout > 1 and bias.stride(0) != 1:
             raise ValueError("bias must be contiguous")
-    rs = cout
     if residual is not None:
-        rs = _row_stride(_require(residual, "residual", like=x, shape=shape), "residual", cout)
+        rs = _row_stride(_require(residual, "residual", dtype, index, shape), "residual", cout)
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
-    ys = _row_stride(_require(out, "out", like=x, shape=shape), "out", cout)
-    rows = out.numel() // cout
-    spec = E.LinearSpec(rows, cin, cout, kind, ACTIVATIONS[activation], xs, ws, rs, ys)
-    with _On(x.device, stream, (x, weight, bias, residual, out)) as s:
-        _check(lib().sscater_linear(ctypes.byref(spec), _ptr(x), _ptr(weight), _ptr(bias), _ptr(residual), _ptr(out), s),
-               "sscater_linear")
+        out, ys = x.new_empty(shape), cout
+    else:
+        ys = _row_stride(_require(out, "out", dtype, index, shape), "out", cout)
+    spec = E.LinearSpec(x.numel() // cin, cin, cout, kind, act, xs, ws, rs, ys)
+    _launch(lib().sscater_linear, "sscater_linear", index, stream, (x, weight, bias, residual, out), spec, x.data_ptr(),
+            weight.data_ptr(), None if bias is None else bias.data_ptr(),
+            None if residual is None else residual.data_ptr(), out.data_ptr())
     return out
 
 
@@ -145,11 +147,10 @@ class Rotary:
         if inv_freq is None:
             table = np.concatenate([base ** (-np.arange(n) / max(n, 1)) for n in self.sections])
             inv_freq = torch.from_numpy(table.astype(np.float32)).to(device)
-        _require(inv_freq, "inv_freq", dtype=torch.float32, shape=(sum(self.sections),))
-        if not inv_freq.is_contiguous():
-            raise ValueError("inv_freq must be contiguous")
+        _dense(inv_freq, "inv_freq", torch.float32, inv_freq.get_device(), (sum(self.sections),))
         self.inv_freq = inv_freq
-        self.interleaved = bool(interleaved)
+        self.interleaved = int(bool(interleaved))
+        self.section = (ctypes.c_int32 * 3)(*self.sections)
 
 
 class TokenCache:
@@ -183,11 +184,10 @@ class TokenCache:
             raise ValueError("k and v come together")
         if k is None:
             k, v = (torch.zeros(shape, dtype=kind, device=device) for _ in range(2))
+        self.index = k.get_device()
         for name, t in (("k", k), ("v", v)):
-            _require(t, name, like=k, dtype=kind, shape=shape)
-            if not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
-        self.k, self.v = k, v
+            _dense(t, name, kind, self.index, shape)
+        self.k, self.v, self.kind = k, v, kind
         self.past = torch.zeros(self.batch, dtype=torch.int64, device=k.device)
         self.seen = 0
 
@@ -210,12 +210,8 @@ class TokenCache:
             if tokens % self.batch or (max_new is not None and max_new * self.batch != tokens):
                 raise ValueError("without start every stream brings the same number of tokens")
             return E.TokenRows(tokens, tokens // self.batch, self.seen, None)
-        _require(start, "start", like=self.past, dtype=torch.int32, shape=(self.batch + 1,))
-        if not start.is_contiguous():
-            raise ValueError("start must be contiguous")
-        if max_new is None:
-            max_new = tokens
-        return E.TokenRows(tokens, max_new, self.seen, start.data_ptr())
+        ptr = _dense(start, "start", torch.int32, self.index, (self.batch + 1,))
+        return E.TokenRows(tokens, tokens if max_new is None else max_new, self.seen, ptr)
 
     def append(self, qkv, pos, rotary: Rotary, q_heads: int, q_weight=None, k_weight=None, eps: float = 1e-6,
                start=None, max_new: Optional[int] = None, out=None, stream=None):
@@ -225,37 +221,29 @@ class TokenCache:
         heads are normalised (root mean square, q_weight and k_weight
         [head_dim]; None: not) and turned by pos (int32 [tokens, axes])."""
         import torch
-        width = (q_heads + 2 * self.kv_heads) * self.head_dim
-        _require(qkv, "qkv", like=self.k)
+        index, dim = self.index, self.head_dim
+        _require(qkv, "qkv", self.kind, index)
         if q_heads < 1 or qkv.dim() != 2:
             raise ValueError("qkv must be [tokens, (q_heads + 2 * kv_heads) * head_dim]")
-        ld = _row_stride(qkv, "qkv", width)
-        tokens = qkv.shape[0]
-        if sum(rotary.sections) * 2 != self.head_dim:
-            raise ValueError("the rotary sections must add up to head_dim / 2")
-        _require(rotary.inv_freq, "inv_freq", like=self.past, dtype=torch.float32)
-        _require(pos, "pos", like=self.past, dtype=torch.int32, shape=(tokens, len(rotary.sections)))
-        if not pos.is_contiguous():
-            raise ValueError("pos must be contiguous")
+        ld = _row_stride(qkv, "qkv", (q_heads + 2 * self.kv_heads) * dim)
+        tokens, axes = qkv.shape[0], len(rotary.sections)
+        freq = _dense(rotary.inv_freq, "inv_freq: head_dim / 2 values,", torch.float32, index, (dim // 2,))
+        at = _dense(pos, "pos", torch.int32, index, (tokens, axes))
         if (q_weight is None) != (k_weight is None):
             raise ValueError("q_weight and k_weight come together")
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None and not _require(w, name, like=self.k, shape=(self.head_dim,)).is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
+        qw = kw = None
+        if q_weight is not None:
+            qw, kw = (_dense(w, "q_weight and k_weight", self.kind, index, (dim,)) for w in (q_weight, k_weight))
         rows = self._rows(tokens, start, max_new)
-        shape = (tokens, q_heads, self.head_dim)
+        shape = (tokens, q_heads, dim)
         if out is None:
-            out = torch.empty(shape, dtype=self.k.dtype, device=self.k.device)
-        elif not _require(out, "out", like=self.k, shape=shape).is_contiguous():
-            raise ValueError("out must be contiguous")
-        section = (ctypes.c_int32 * 3)(*rotary.sections)
-        spec = E.HeadSpec(q_heads, len(rotary.sections), section, int(rotary.interleaved), eps, ld)
-        cache = self._spec()
-        tensors = (qkv, pos, rotary.inv_freq, q_weight, k_weight, start, out, self.k, self.v, self.past)
-        with _On(self.k.device, stream, tensors) as s:
-            _check(lib().sscater_tokens_append(ctypes.byref(spec), ctypes.byref(cache), ctypes.byref(rows), _ptr(qkv),
-                                               _ptr(q_weight), _ptr(k_weight), _ptr(rotary.inv_freq), _ptr(pos),
-                                               _ptr(out), s), "sscater_tokens_append")
+            out = qkv.new_empty(shape)
+        else:
+            _dense(out, "out", self.kind, index, shape)
+        spec = E.HeadSpec(q_heads, axes, rotary.section, rotary.interleaved, eps, ld)
+        _launch(lib().sscater_tokens_append, "sscater_tokens_append", index, stream,
+                (qkv, pos, rotary.inv_freq, q_weight, k_weight, start, out, self.k, self.v, self.past), spec,
+                self._spec(), rows, qkv.data_ptr(), qw, kw, freq, at, out.data_ptr())
         return out
 
     def attend(self, q, window: int, start=None, max_new: Optional[int] = None, causal: bool = True,
@@ -265,8 +253,8 @@ class TokenCache:
         sees the `window` newest tokens up to itself and the sinks (causal), or
         every new token of its stream and the window before them (not causal).
         scale: 1 / sqrt(head_dim) unless given."""
-        import torch
-        _require(q, "q", like=self.k)
+        index = self.index
+        _require(q, "q", self.kind, index)
         if q.dim() != 3 or q.shape[2] != self.head_dim or q.shape[1] < 1 or q.shape[1] % self.kv_heads:
             raise ValueError("q must be [tokens, q_heads, head_dim], q_heads a multiple of kv_heads")
         if not q.is_contiguous() or q.data_ptr() % 16:
@@ -275,25 +263,24 @@ class TokenCache:
             raise ValueError("window must be at least 1")
         rows = self._rows(q.shape[0], start, max_new)
         if out is None:
-            out = torch.empty_like(q)
-        elif not _require(out, "out", like=q, shape=q.shape).is_contiguous() or out.data_ptr() % 16:
-            raise ValueError("out must be contiguous, on a 16-byte boundary")
-        spec = E.AttendSpec(q.shape[1], min(int(window), 2 ** 31 - 1), int(bool(causal)),
-                            self.head_dim ** -0.5 if scale is None else float(scale))
-        cache = self._spec()
-        need = ctypes.c_size_t()
-        args = (ctypes.byref(spec), ctypes.byref(cache), ctypes.byref(rows))
-        _check(lib().sscater_tokens_workspace(*args, ctypes.byref(need)), "sscater_tokens_workspace")
-        work = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
-        with _On(q.device, stream, (q, start, out, work, self.k, self.v, self.past)) as s:
-            _check(lib().sscater_tokens_attend(*args, _ptr(q), _ptr(out), _ptr(work), need.value, s),
-                   "sscater_tokens_attend")
+            out = q.new_empty(q.shape)
+        elif _dense(out, "out", self.kind, index, q.shape) % 16:
+            raise ValueError("out must be on a 16-byte boundary")
+        spec = E.AttendSpec(q.shape[1], min(int(window), 2 ** 31 - 1), 1 if causal else 0,
+                            self.head_dim ** -0.5 if scale is None else scale)
+        cache, need, work = self._spec(), ctypes.c_size_t(), None
+        _check(lib().sscater_tokens_workspace(spec, cache, rows, need), "sscater_tokens_workspace")
+        if need.value:
+            import torch
+            work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        _launch(lib().sscater_tokens_attend, "sscater_tokens_attend", index, stream,
+                (q, start, out, work, self.k, self.v, self.past), spec, cache, rows, q.data_ptr(), out.data_ptr(),
+                None if work is None else work.data_ptr(), need.value)
         return out
 
     def advance(self, tokens: int, start=None, max_new: Optional[int] = None, stream=None) -> None:
         """The call's tokens become past ones."""
         rows = self._rows(int(tokens), start, max_new)
-        cache = self._spec()
-        with _On(self.past.device, stream, (start, self.past)) as s:
-            _check(lib().sscater_tokens_advance(ctypes.byref(cache), ctypes.byref(rows), s), "sscater_tokens_advance")
+        _launch(lib().sscater_tokens_advance, "sscater_tokens_advance", self.index, stream, (start, self.past),
+                self._spec(), rows)
         self.seen += rows.max_new
