@@ -13,6 +13,9 @@
 #include "../../include/sscater.h"
 #include "device_common.h"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace ssc {
 
 typedef float f16v __attribute__((ext_vector_type(16)));
@@ -27,33 +30,61 @@ struct LinearArgs {
     int K, N, act;
     int tn;               // tiles across the output channels
     int tiles, per_xcd;   // all tiles, and those of an XCD (workgroup b runs on XCD b % 8)
+    int packed;           // the output's rows lie one behind the other, in one tile, on a 16-byte boundary
     int rvec, yvec;       // residual and output rows may be accessed 16 bytes at a time
 };
 
-// Up to this many rows take linear_rows_kernel.
-constexpr int ROWS_KERNEL = 64;
+// Fewer tiles of 64 x 64 than these take linear_rows_kernel.
+constexpr int FEW_TILES = 160;
 
 // What a copy reads where its tile has nothing.
 __device__ __attribute__((aligned(16))) uint32_t linear_zero[4];
 
-// z (1 + erf(z / sqrt 2)) / 2, with erfc(t) = exp(-t^2) p(1 / (1 + 0.3275911 t))
-// for t >= 0 (Abramowitz and Stegun 7.1.26, |error| <= 1.5e-7).
+// z (1 + erf(z / sqrt 2)) / 2 = max(z, 0) - |z| Phi(-|z|), with log2 Phi(-t) as a
+// polynomial in t (fitted for 0 <= t <= 5.5 by weighted least squares, the
+// weights moved until Phi's error was level): |error of Phi| <= 4e-8, which is
+// also what stays from there on.  60 clocks of a wavefront, 16 of them the one
+// transcendental instruction; the layers that end in it are bound by this.  (By
+// erfc's rational approximation in 1 / (1 + p t) 80.)
 __device__ __forceinline__ float gelu(float z) {
-    const float t = fabsf(z) * 0.70710678f;
-    const float u = __builtin_amdgcn_rcpf(fmaf(0.3275911f, t, 1.f));
-    float p = fmaf(1.061405429f, u, -1.453152027f);
-    p = fmaf(p, u, 1.421413741f);
-    p = fmaf(p, u, -0.284496736f);
-    p = fmaf(p, u, 0.254829592f) * u;
-    const float half = 0.5f * z * (p * __builtin_amdgcn_exp2f(-1.44269504f * t * t));
-    return z >= 0.f ? z - half : half;
+    const float t = fminf(fabsf(z), 5.5f);
+    float p = fmaf(8.470141e-06f, t, -5.3903543e-05f);
+    p = fmaf(p, t, -4.212365e-04f);
+    p = fmaf(p, t, 7.389273e-03f);
+    p = fmaf(p, t, -5.2691113e-02f);
+    p = fmaf(p, t, -4.5915315e-01f);
+    p = fmaf(p, t, -1.15111089f);
+    p = fmaf(p, t, -0.99999988f);
+    return fmaf(-t, __builtin_amdgcn_exp2f(p), z < 0.f ? 0.f : z);
 }
 
-__device__ __forceinline__ float activate(float z, int act) {
-    if (act == SSCATER_ACT_RELU) return z < 0.f ? 0.f : z;
-    if (act == SSCATER_ACT_GELU) return fabsf(z) > 1e30f ? fmaxf(z, 0.f) : gelu(z);
-    if (act == SSCATER_ACT_SILU) return z / (1.f + __expf(-z));
+typedef __attribute__((address_space(3))) float lds_float;
+
+template <int ACT>
+using Act = std::integral_constant<int, ACT>;
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+    if constexpr (ACT == SSCATER_ACT_RELU) return z < 0.f ? 0.f : z;
+    if constexpr (ACT == SSCATER_ACT_GELU) return gelu(z);
+    if constexpr (ACT == SSCATER_ACT_SILU)
+        return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z));
     return z;
+}
+
+// N values of one activation, chosen once for all of them.
+template <int N>
+__device__ __forceinline__ void activate_all(float (&z)[N], int act) {
+    if (act == SSCATER_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = activate<SSCATER_ACT_RELU>(z[e]);
+    } else if (act == SSCATER_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = activate<SSCATER_ACT_GELU>(z[e]);
+    } else if (act == SSCATER_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) z[e] = activate<SSCATER_ACT_SILU>(z[e]);
+    }
 }
 
 template <bool F32>
@@ -80,13 +111,34 @@ __device__ __forceinline__ f16v mfma32(uint4 a, uint4 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, B, c, 0, 0, 0);
 }
 
+// Channels k.. of a row that starts at value `at` and may be aligned to its values
+// only: 16 bytes, zeros from channel K on.
+template <bool F32>
+__device__ __forceinline__ uint4 load_piece(const void* base, int64_t at, int k, int K) {
+    constexpr int E = F32 ? 4 : 8;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (k + E <= K) {
+        __builtin_memcpy(&v, (const char*)base + (at + k) * (F32 ? 4 : 2), 16);
+    } else if (k < K) {
+        uint32_t b[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (k + e >= K) continue;
+            if constexpr (F32) b[e] = ((const uint32_t*)base)[at + k + e];
+            else b[e / 2] |= (uint32_t)((const uint16_t*)base)[at + k + e] << (16 * (e & 1));
+        }
+        v = make_uint4(b[0], b[1], b[2], b[3]);
+    }
+    return v;
+}
+
 // 16-byte piece `piece` of tile row `row` in LDS: rows of RB bytes, the pieces
 // of neighbouring rows moved so that lanes which read one piece of eight rows
 // fall on different banks.
 template <int RB>
 __device__ __forceinline__ int place(int row, int piece) {
-    if constexpr (RB == 64) return row * 64 + ((piece ^ (row >> 1)) & 3) * 16;
-    return row * 128 + ((piece ^ row) & 7) * 16;
+    if constexpr (RB == 64) return row * 64 + ((piece ^ (row >> 2)) & 3) * 16;
+    return row * 128 + ((piece ^ (row >> 1)) & 7) * 16;
 }
 
 // One K step of an operand tile as 16-byte pieces in registers, for rows that
@@ -106,14 +158,7 @@ struct Staged {
                 v[i] = make_uint4(0, 0, 0, 0);
                 if (k < K) v[i] = *(const uint4*)((const char*)base + (row * ld + k) * (F32 ? 4 : 2));
             } else {
-                uint32_t b[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    if (k + e >= K) continue;
-                    if constexpr (F32) b[e] = ((const uint32_t*)base)[row * ld + k + e];
-                    else b[e / 2] |= (uint32_t)((const uint16_t*)base)[row * ld + k + e] << (16 * (e & 1));
-                }
-                v[i] = make_uint4(b[0], b[1], b[2], b[3]);
+                v[i] = load_piece<F32>(base, row * ld, k, K);
             }
         }
     }
@@ -144,78 +189,197 @@ struct Staged {
 };
 
 // The same straight into LDS (bf16 rows on 16-byte boundaries): a copy is 1 KB,
-// the four wavefronts take them in turn.
-template <int ROWS, int P>
-__device__ __forceinline__ void copy_tile(lds_char* lds, const void* base, int64_t ld, int64_t row0, int64_t rows,
-                                          int k0, int K) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// the wavefronts take them in turn.  A lane's rows and pieces are the same
+// in every K step, so their offsets from the tile's first value are formed once,
+// in 32 bits (the host sees to it that they fit), and a step only moves the
+// uniform base: with the addresses formed anew the vector instructions around
+// the copies took longer than the matrix instructions.
+template <int ROWS, int P, int WAVES = 4>
+struct Copied {
+    static constexpr int N = ROWS * P / 64 / WAVES;
+    const char* base;
+    uint32_t off[N];
+    __device__ __forceinline__ void init(const void* p, int64_t ld, int64_t row0, int64_t rows) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        base = (const char*)p + row0 * ld * 2;
+        const int most = (int)min((int64_t)ROWS, rows - row0) - 1;
 #pragma unroll
-    for (int i = 0; i < ROWS * P / 256; ++i) {
-        const int c = i * 4 + wave;
-        const int row = c * (64 / P) + lane / P;
-        const int piece = (lane % P) ^ (P == 4 ? (row >> 1) & 3 : row & 7);
-        const int k = k0 + piece * 8;
-        const char* src = (const char*)base + (min(row0 + row, rows - 1) * ld + k) * 2;
-        copy16(k < K ? src : (const char*)linear_zero, lds + c * 1024);
+        for (int i = 0; i < N; ++i) {
+            const int row = (i * WAVES + wave) * (64 / P) + lane / P;
+            off[i] = (uint32_t)min(row, most) * (uint32_t)(ld * 2) + piece(row) * 16;
+        }
+    }
+    static __device__ __forceinline__ int piece(int row) {
+        return ((int)threadIdx.x % P) ^ ((row >> 1) & 7);
+    }
+    // copy i of the K step from channel k
+    __device__ __forceinline__ void one(lds_char* lds, int i, int k, int K) const {
+        const int wave = threadIdx.x >> 6;
+        const char* from = base + (int64_t)k * 2 + off[i];
+        if (k + P * 8 > K) {
+            const int row = (i * WAVES + wave) * (64 / P) + (threadIdx.x & 63) / P;
+            if (k + piece(row) * 8 >= K) from = (const char*)linear_zero;
+        }
+        copy16(from, lds + (i * WAVES + wave) * 1024);
+    }
+    __device__ __forceinline__ void copy(lds_char* lds, int k, int K) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) one(lds, i, k, K);
+    }
+};
+
+// One block of sums on its way out where the tile hangs over an edge or rows may
+// not be accessed 16 bytes at a time: the lane's row m, its channels n + 8 g +
+// 4 h + 0..3 (g = 0..3), with bias, activation, residual and rounding.
+template <bool F32, int ACT>
+__device__ __forceinline__ void put_edge(const LinearArgs& a, const f16v& acc, const lds_float* bias, int64_t m, int n,
+                                         int h) {
+    if (m >= a.M) return;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int c = 8 * (e >> 2) + 4 * h + (e & 3);
+        if (n + c >= a.N) continue;
+        float z = activate<ACT>(acc[e] + bias[c]);
+        if (a.res) z += load_value<F32>(a.res, m * a.ldr + n + c);
+        if constexpr (F32) ((float*)a.y)[m * a.ldy + n + c] = z;
+        else ((uint16_t*)a.y)[m * a.ldy + n + c] = (uint16_t)bf16_pair(z, z);
     }
 }
 
-// E values of a row: bias, activation, residual, rounding.
-template <bool F32>
-__device__ __forceinline__ void finish(const LinearArgs& a, float (&z)[8], const float (&bias)[8], int64_t m, int n) {
-    constexpr int E = 8;
-#pragma unroll
-    for (int e = 0; e < E; ++e) z[e] += bias[e];
-    if (a.act == SSCATER_ACT_RELU) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) z[e] = activate(z[e], SSCATER_ACT_RELU);
-    } else if (a.act == SSCATER_ACT_GELU) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) z[e] = activate(z[e], SSCATER_ACT_GELU);
-    } else if (a.act == SSCATER_ACT_SILU) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) z[e] = activate(z[e], SSCATER_ACT_SILU);
-    }
-    const bool whole = n + E <= a.N;
+// 32 rows of NI blocks inside the matrix.  They pass through 32 * RB bytes of LDS
+// that are the wavefront's own, so that 4 or 8 lanes store one row's bytes
+// together (straight from the sums' layout a store is 32 rows of 32 bytes, which
+// the memory path takes at a quarter of its rate), and the residual comes the
+// other way through the same place.  bf16: lanes r and r + 32 hold the two halves
+// of eight channels and swap halves of two groups first.
+template <bool F32, int ACT, int NI>
+__device__ __forceinline__ void put_rows(const LinearArgs& a, const f16v (&acc)[NI], const lds_float* bias,
+                                         lds_char* own, int64_t m, int n) {
+    constexpr int S = F32 ? 4 : 2, RB = 32 * NI * S, L = RB / 16, RPI = 64 / L;   // lanes of a row, rows of a store
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+    typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+    typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) u4v lds_u4v;
+    typedef __attribute__((address_space(3))) u2v lds_u2v;
     if (a.res) {
-        if (whole && a.rvec) {
-            if constexpr (F32) {
-                const float4* r = (const float4*)((const float*)a.res + m * a.ldr + n);
-                const float4 r0 = r[0], r1 = r[1];
-                z[0] += r0.x; z[1] += r0.y; z[2] += r0.z; z[3] += r0.w;
-                z[4] += r1.x; z[5] += r1.y; z[6] += r1.z; z[7] += r1.w;
-            } else {
-                const uint4 r = *(const uint4*)((const uint16_t*)a.res + m * a.ldr + n);
-                const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+        const char* from = (const char*)a.res + ((m + lane / L) * a.ldr + n) * S + lane % L * 16;
+        u4v v[32 / RPI];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    z[2 * e] += __uint_as_float(w[e] << 16);
-                    z[2 * e + 1] += __uint_as_float(w[e] & 0xFFFF0000u);
+        for (int i = 0; i < 32 / RPI; ++i) v[i] = *(const u4v*)(from + (int64_t)i * RPI * a.ldr * S);
+#pragma unroll
+        for (int i = 0; i < 32 / RPI; ++i) *(lds_u4v*)(own + place<RB>(i * RPI + lane / L, lane % L)) = v[i];
+    }
+    u4v out[NI][4 * S / 4];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+        float z[16];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f4v b = *(const __attribute__((address_space(3))) f4v*)(bias + 32 * i + 8 * g + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[4 * g + e] = activate<ACT>(acc[i][4 * g + e] + b[e]);
+        }
+        if (a.res) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                if constexpr (F32) {
+                    const u4v v = *(const lds_u4v*)(own + place<RB>(r, 8 * i + 2 * g + h));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[4 * g + e] += __uint_as_float(v[e]);
+                } else {
+                    const u2v v = *(const lds_u2v*)(own + place<RB>(r, 4 * i + g) + 8 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        z[4 * g + e] += __uint_as_float(e & 1 ? v[e / 2] & 0xFFFF0000u : v[e / 2] << 16);
                 }
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (n + e < a.N) z[e] += load_value<F32>(a.res, m * a.ldr + n + e);
         }
-    }
-    if (whole && a.yvec) {
         if constexpr (F32) {
-            float4* y = (float4*)((float*)a.y + m * a.ldy + n);
-            y[0] = make_float4(z[0], z[1], z[2], z[3]);
-            y[1] = make_float4(z[4], z[5], z[6], z[7]);
-        } else {
-            *(uint4*)((uint16_t*)a.y + m * a.ldy + n) = make_uint4(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]),
-                                                                   bf16_pair(z[4], z[5]), bf16_pair(z[6], z[7]));
-        }
-    } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (n + e < a.N) {
-                if constexpr (F32) ((float*)a.y)[m * a.ldy + n + e] = z[e];
-                else ((uint16_t*)a.y)[m * a.ldy + n + e] = (uint16_t)bf16_pair(z[e], z[e]);
+            for (int g = 0; g < 4; ++g)
+                out[i][g] = u4v{__float_as_uint(z[4 * g]), __float_as_uint(z[4 * g + 1]), __float_as_uint(z[4 * g + 2]),
+                                __float_as_uint(z[4 * g + 3])};
+        } else {
+#pragma unroll
+            for (int g = 0; g < 4; g += 2) {
+                const auto lo = __builtin_amdgcn_permlane32_swap(bf16_pair(z[4 * g], z[4 * g + 1]),
+                                                                 bf16_pair(z[4 * g + 4], z[4 * g + 5]), false, false);
+                const auto hi = __builtin_amdgcn_permlane32_swap(bf16_pair(z[4 * g + 2], z[4 * g + 3]),
+                                                                 bf16_pair(z[4 * g + 6], z[4 * g + 7]), false, false);
+                out[i][g / 2] = u4v{lo[0], hi[0], lo[1], hi[1]};
             }
+        }
     }
+    // the residual's reads above and these writes are of one wavefront, in order
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int g = 0; g < S; ++g) *(lds_u4v*)(own + place<RB>(r, 2 * S * i + 2 * g + h)) = out[i][g];
+    char* to = (char*)a.y + ((m + lane / L) * a.ldy + n) * S + lane % L * 16;
+#pragma unroll
+    for (int i = 0; i < 32 / RPI; ++i)
+        *(u4v*)(to + (int64_t)i * RPI * a.ldy * S) = *(const lds_u4v*)(own + place<RB>(i * RPI + lane / L, lane % L));
+}
+
+// 32 rows of a matrix of few channels that lie one behind the other (no more than
+// the wavefront's 32 * NI channels, y_stride = cout): put together in LDS as they
+// lie in memory and stored 16 bytes a lane.  32 * N * S bytes are whole pieces.
+template <bool F32, int ACT, int NI>
+__device__ __forceinline__ void put_packed(const LinearArgs& a, const f16v (&acc)[NI], const lds_float* bias,
+                                           lds_char* own, int64_t m) {
+    constexpr int S = F32 ? 4 : 2;
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int c = 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
+            if (c >= a.N) continue;
+            float z = activate<ACT>(acc[i][e] + bias[c]);
+            if (a.res) z += load_value<F32>(a.res, (m + r) * a.ldr + c);
+            lds_char* to = own + (r * a.N + c) * S;
+            if constexpr (F32) *(__attribute__((address_space(3))) float*)to = z;
+            else *(__attribute__((address_space(3))) uint16_t*)to = (uint16_t)bf16_pair(z, z);
+        }
+    char* y = (char*)a.y + m * a.N * S;
+    for (int i = lane; i < 2 * a.N * S; i += 64) *(uint4*)(y + i * 16) = lds16(own + i * 16);
+}
+
+// A wavefront's TM x TN blocks; own: 4 KB of LDS that no other wavefront uses.
+template <bool F32, int ACT, bool FULL, int TM, int TN>
+__device__ __forceinline__ void put_blocks(const LinearArgs& a, const f16v (&acc)[TN][TM], const lds_float* bias,
+                                           lds_char* own, int64_t m, int n) {
+    const int r = threadIdx.x & 31, h = threadIdx.x >> 5 & 1;
+    constexpr int NI = !F32 && TN % 2 == 0 ? 2 : 1;
+#pragma unroll
+    for (int j = 0; j < TM; ++j)
+#pragma unroll
+        for (int i = 0; i < TN; i += NI) {
+            if constexpr (FULL) {
+                f16v z[NI];
+#pragma unroll
+                for (int c = 0; c < NI; ++c) z[c] = acc[i + c][j];
+                put_rows<F32, ACT, NI>(a, z, bias + 32 * i, own, m + 32 * j, n + 32 * i);
+            } else {
+#pragma unroll
+                for (int c = 0; c < NI; ++c)
+                    put_edge<F32, ACT>(a, acc[i + c][j], bias + 32 * (i + c), m + 32 * j + r, n + 32 * (i + c), h);
+            }
+        }
+}
+
+// put(activation, full) with both as types, chosen once for a tile.
+template <typename Put>
+__device__ __forceinline__ void put_tile(const LinearArgs& a, bool inside, const Put& put) {
+    const bool full = inside && a.yvec && (a.rvec || !a.res);
+    auto all = [&](auto f) __attribute__((always_inline)) {
+        if (a.act == SSCATER_ACT_NONE) put(Act<SSCATER_ACT_NONE>{}, f);
+        else if (a.act == SSCATER_ACT_RELU) put(Act<SSCATER_ACT_RELU>{}, f);
+        else if (a.act == SSCATER_ACT_GELU) put(Act<SSCATER_ACT_GELU>{}, f);
+        else put(Act<SSCATER_ACT_SILU>{}, f);
+    };
+    if (full) all(std::true_type{});
+    else all(std::false_type{});
 }
 
 // A wavefront owns TM x TN blocks of 32 rows x 32 output channels, the
@@ -224,14 +388,12 @@ template <bool F32, bool VEC, int WM, int WN, int TM, int TN>
 struct LinearShape {
     static constexpr int BM = 32 * WM * TM, BN = 32 * WN * TN;
     static constexpr bool COPY = VEC && !F32;          // straight into LDS
-    static constexpr int P = F32 ? 8 : 8;              // 16-byte pieces of a row's K step
+    static constexpr int P = 8;          // 16-byte pieces of a row's K step
     static constexpr int BK = P * (F32 ? 4 : 8);       // 32 or 64 channels
     static constexpr int SX = F32 ? BM * 64 * 3 : BM * 16 * P;
     static constexpr int SW = F32 ? BN * 64 * 3 : BN * 16 * P;
     static constexpr int NST = COPY ? 2 : 1;           // stages in LDS
-    static constexpr int PITCH = 32 * TN + 4;          // floats of a row on the way out
-    static constexpr int OUT = 4 * 32 * PITCH * 4;
-    static constexpr int LDS = NST * (SX + SW) > OUT ? NST * (SX + SW) : OUT;
+    static constexpr int LDS = NST * (SX + SW) > 16384 ? NST * (SX + SW) : 16384;
 };
 
 template <bool F32, bool VEC, int WM, int WN, int TM, int TN>
@@ -246,6 +408,10 @@ __global__ __launch_bounds__(256, 2) void linear_kernel(LinearArgs a) {
     const int n0 = (id % a.tn) * C::BN;
     const int wm = wave % WM * (32 * TM), wn = wave / WM * (32 * TN);
     const int r = lane & 31, h = lane >> 5;
+    // read after the K loop's barriers
+    __shared__ __attribute__((aligned(16))) float bias[C::BN];
+    if ((int)threadIdx.x < C::BN)
+        bias[threadIdx.x] = a.bias && n0 + (int)threadIdx.x < a.N ? load_value<F32>(a.bias, n0 + threadIdx.x) : 0.f;
     f16v acc[TN][TM];
 #pragma unroll
     for (int i = 0; i < TN; ++i)
@@ -290,12 +456,16 @@ __global__ __launch_bounds__(256, 2) void linear_kernel(LinearArgs a) {
 
     if constexpr (C::COPY) {
         constexpr int CP = (C::BM + C::BN) * C::P / 256;     // copies of a wavefront per stage
-        auto issue = [&](int step) __attribute__((always_inline)) {
-            lds_char* to = lds + (step & 1) * (C::SX + C::SW);
-            copy_tile<C::BM, C::P>(to, a.x, a.ldx, m0, a.M, step * C::BK, a.K);
-            copy_tile<C::BN, C::P>(to + C::SX, a.w, a.ldw, n0, a.N, step * C::BK, a.K);
-        };
+        Copied<C::BM, C::P> x;
+        Copied<C::BN, C::P> w;
+        x.init(a.x, a.ldx, m0, a.M);
+        w.init(a.w, a.ldw, n0, a.N);
         const int steps = (a.K + C::BK - 1) / C::BK;
+        auto issue = [&](int k) __attribute__((always_inline)) {
+            lds_char* to = lds + (k & 1) * (C::SX + C::SW);
+            x.copy(to, k * C::BK, a.K);
+            w.copy(to + C::SX, k * C::BK, a.K);
+        };
         issue(0);
         for (int k = 0; k < steps; ++k) {
             if (k + 1 < steps) {
@@ -310,6 +480,8 @@ __global__ __launch_bounds__(256, 2) void linear_kernel(LinearArgs a) {
             lds_barrier();
         }
     } else {
+        // the next step is under way in registers beside the products (__syncthreads would wait for it; two or three
+        // steps ahead took as long)
         Staged<F32, VEC, C::BM, C::P> x;
         Staged<F32, VEC, C::BN, C::P> w;
         x.load(a.x, a.ldx, m0, a.M, 0, a.K);
@@ -317,120 +489,270 @@ __global__ __launch_bounds__(256, 2) void linear_kernel(LinearArgs a) {
         for (int k0 = 0; k0 < a.K; k0 += C::BK) {
             x.store(lds);
             w.store(lds + C::SX);
-            __syncthreads();
+            lds_barrier();
             if (k0 + C::BK < a.K) {
                 x.load(a.x, a.ldx, m0, a.M, k0 + C::BK, a.K);
                 w.load(a.w, a.ldw, n0, a.N, k0 + C::BK, a.K);
             }
             multiply(lds, lds + C::SX);
-            __syncthreads();
+            lds_barrier();
         }
     }
 
-    // On the way out the wavefront's sums pass through its own part of LDS, 32
-    // rows at a time, so that a row's channels are stored together.
-    constexpr int G = 4 * TN;                          // lanes of a row
-    float* t = (float*)lds_ + wave * 32 * C::PITCH;
-    const int n = n0 + wn + lane % G * 8;
-    float bias[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bias[e] = a.bias && n + e < a.N ? load_value<F32>(a.bias, n + e) : 0.f;
-#pragma unroll
-    for (int j = 0; j < TM; ++j) {
-        const int64_t mb = m0 + wm + 32 * j;
+    if constexpr (F32) {
+        // an infinity leaves a NaN in its lower planes: such sums are formed again from the values
+        bool bad = false;
 #pragma unroll
         for (int i = 0; i < TN; ++i)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                float z[4];
+            for (int j = 0; j < TM; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    z[e] = acc[i][j][4 * g + e];
-                    const int nn = n0 + wn + 32 * i + 8 * g + 4 * h + e;
-                    if (F32 && z[e] != z[e] && nn < a.N && mb + r < a.M) {
-                        // an infinity leaves a NaN in its lower planes: such a sum is formed again from the values
-                        z[e] = 0.f;
+                for (int e = 0; e < 16; ++e) bad |= acc[i][j][e] != acc[i][j][e];
+        if (__ballot(bad) != 0) {
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int j = 0; j < TM; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int64_t m = m0 + wm + 32 * j + r;
+                        const int n = n0 + wn + 32 * i + 8 * (e >> 2) + 4 * h + (e & 3);
+                        if (acc[i][j][e] == acc[i][j][e] || m >= a.M || n >= a.N) continue;
+                        float z = 0.f;
                         for (int k = 0; k < a.K; ++k)
-                            z[e] = fmaf(load_value<F32>(a.x, (mb + r) * a.ldx + k), load_value<F32>(a.w, nn * a.ldw + k),
-                                        z[e]);
+                            z = fmaf(load_value<F32>(a.x, m * a.ldx + k), load_value<F32>(a.w, n * a.ldw + k), z);
+                        acc[i][j][e] = z;
+                    }
+        }
+    }
+    auto put = [&](auto act, auto full) __attribute__((always_inline)) {
+        lds_char* own = lds + wave * (C::LDS / 4);
+        if constexpr (WN == 1 && !decltype(full)::value) {
+            if (a.packed) {
+#pragma unroll
+                for (int j = 0; j < TM; ++j) {
+                    const int64_t m = m0 + wm + 32 * j;
+                    f16v z[TN];
+#pragma unroll
+                    for (int i = 0; i < TN; ++i) z[i] = acc[i][j];
+                    if (m + 32 <= a.M) {
+                        put_packed<F32, decltype(act)::value, TN>(a, z, (const lds_float*)bias, own, m);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < TN; ++i)
+                            put_edge<F32, decltype(act)::value>(a, z[i], (const lds_float*)bias + 32 * i, m + r, 32 * i, h);
                     }
                 }
-                *(float4*)(t + r * C::PITCH + 32 * i + 8 * g + 4 * h) = make_float4(z[0], z[1], z[2], z[3]);
+                return;
             }
-#pragma unroll
-        for (int p = 0; p < 32 / (64 / G); ++p) {
-            const int row = p * (64 / G) + lane / G;
-            const float4 z0 = *(const float4*)(t + row * C::PITCH + lane % G * 8);
-            const float4 z1 = *(const float4*)(t + row * C::PITCH + lane % G * 8 + 4);
-            float z[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
-            if (mb + row < a.M && n < a.N) finish<F32>(a, z, bias, mb + row, n);
         }
+        put_blocks<F32, decltype(act)::value, decltype(full)::value, TM, TN>(a, acc, (const lds_float*)bias + wn, own,
+                                                                             m0 + wm, n0 + wn);
+    };
+    put_tile(a, m0 + C::BM <= a.M && n0 + C::BN <= a.N, put);
+}
+
+// Many rows and channels, bf16: persistent workgroups of eight wavefronts, one
+// on a compute unit, each with tiles of 256 rows x 128 channels (a wavefront
+// 64 x 64) one after the other.  K steps of 64 channels go through three LDS
+// stages of 48 KB, copied two steps ahead, and on from the end of one tile into
+// the next, so that a tile starts on operands that are there already.
+//
+// Why: a copy takes about 1100 clocks to arrive, 57 KB have to be under way on a
+// compute unit to have its 52 bytes a clock from L2 all the time, and one tile's
+// first copies come from HBM; as separate workgroups of 128 x 128 with two
+// stages the tiles spent half of their time on their first step and their way
+// out.  256 x 128 needs 923 clocks of copies for the 1024 of matrix
+// instructions in a step.
+//
+// The tiles of an XCD are a range with the channels going fastest, so that its
+// workgroups' rows meet in its L2.  The stages of the next tile are awaited before
+// this one's stores are issued: counted among younger stores they could not be.
+struct BigShape {
+    static constexpr int BM = 256, BN = 128, P = 8, BK = 64, WAVES = 8;
+    static constexpr int SX = BM * 128, SW = BN * 128, STAGE = SX + SW, NST = 3;
+};
+
+__global__ __launch_bounds__(512) void linear_big_kernel(LinearArgs a) {
+    using C = BigShape;
+    __shared__ __attribute__((aligned(1024))) char lds_[C::NST * C::STAGE];
+    __shared__ __attribute__((aligned(16))) float bias[2][C::BN];
+    lds_char* lds = (lds_char*)lds_;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = lane & 31, h = lane >> 5;
+    const int wm = wave % 4 * 64, wn = wave / 4 * 64;
+    const int first = (int)(blockIdx.x & 7) * a.per_xcd + (int)(blockIdx.x >> 3);
+    const int end = min(a.tiles, ((int)(blockIdx.x & 7) + 1) * a.per_xcd), stride = (int)(gridDim.x >> 3);
+    const int steps = (a.K + C::BK - 1) / C::BK;
+    constexpr int CP = (C::BM + C::BN) * C::P / 64 / C::WAVES;   // copies of a wavefront per stage
+
+    // what is copied next
+    Copied<C::BM, C::P, C::WAVES> x;
+    Copied<C::BN, C::P, C::WAVES> w;
+    int tile = first, at = 0, fill = 0;
+    auto begin = [&]() __attribute__((always_inline)) {
+        x.init(a.x, a.ldx, (int64_t)(tile / a.tn) * C::BM, a.M);
+        w.init(a.w, a.ldw, (int64_t)(tile % a.tn) * C::BN, a.N);
+    };
+    // the copies of a step in four parts, between its products: all at once they
+    // keep the wavefronts from their products until the memory path has taken them
+    auto issue = [&](int part) __attribute__((always_inline)) {
+        if (tile < end) {
+            lds_char* to = lds + fill * C::STAGE;
+            x.one(to, part, at * C::BK, a.K);
+            if (part < 2) w.one(to + C::SX, part, at * C::BK, a.K);
+        }
+        if (part == 3) {
+            if (tile < end && ++at == steps) {
+                at = 0;
+                tile += stride;
+                if (tile < end) begin();
+            }
+            fill = fill + 1 == C::NST ? 0 : fill + 1;
+        }
+    };
+    if (first >= end) return;
+    begin();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) issue(i & 3);
+    wait_vm<0>();
+    int slot = 0, side = 0;
+    for (int t = first; t < end; t += stride, side ^= 1) {
+        const int64_t m0 = (int64_t)(t / a.tn) * C::BM;
+        const int n0 = t % a.tn * C::BN;
+        if ((int)threadIdx.x < C::BN)
+            bias[side][threadIdx.x] =
+                a.bias && n0 + (int)threadIdx.x < a.N ? load_value<false>(a.bias, n0 + threadIdx.x) : 0.f;
+        f16v acc[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = f16v{};
+        for (int k = 0; k < steps; ++k) {
+            // the first two steps of a tile were awaited before the last one's stores; later ones have one younger stage
+            // behind them, or none at the end of the last tile
+            if (k >= 2) {
+                if (tile < end || k + 1 < steps) wait_vm<CP>();
+                else wait_vm<0>();
+            }
+            lds_barrier();
+            const lds_char* X = lds + slot * C::STAGE;
+            const lds_char* W = X + C::SX;
+            uint4 xv[2][2], wv[2][2];
+            auto take = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    xv[s & 1][j] = lds16(X + place<128>(wm + 32 * j + r, 2 * s + h));
+                    wv[s & 1][j] = lds16(W + place<128>(wn + 32 * j + r, 2 * s + h));
+                }
+            };
+            take(0);
+#pragma unroll
+            for (int s = 0; s < C::BK / 16; ++s) {
+                if (s < 3) take(s + 1);
+                issue(s);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = mfma32(wv[s & 1][i], xv[s & 1][j], acc[i][j]);
+            }
+            slot = slot + 1 == C::NST ? 0 : slot + 1;
+        }
+        wait_vm<0>();
+        // the stage read last takes no copies before the next barrier but one
+        lds_barrier();
+        lds_char* own = lds + (slot == 0 ? C::NST - 1 : slot - 1) * C::STAGE + wave * 4096;
+        auto put = [&](auto act, auto full) __attribute__((always_inline)) {
+            put_blocks<false, decltype(act)::value, decltype(full)::value, 2, 2>(
+                a, acc, (const lds_float*)bias[side] + wn, own, m0 + wm, n0 + wn);
+        };
+        put_tile(a, m0 + C::BM <= a.M && n0 + C::BN <= a.N, put);
     }
 }
 
-// Few rows: a workgroup owns 16 rows x 16 output channels and its wavefronts
+// Few rows: a workgroup owns 16 T rows x 16 T output channels and its wavefronts
 // share K, each with its operands straight from memory, so that a call is one
 // round trip and a sum through LDS.  fp32 takes the fp32 matrix instructions.
-template <bool F32, bool VEC>
+template <bool F32, bool VEC, int T>
 __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a) {
     constexpr int E = F32 ? 4 : 8, BK = 4 * E;         // channels of a lane, and of a wavefront's piece
-    __shared__ float sums[4][4][64];
+    __shared__ float sums[4][T * T * 4][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n0 = (int)(blockIdx.x % a.tn) * 16;
-    const int64_t m0 = (int64_t)(blockIdx.x / a.tn) * 16;
-    const int64_t n = min(n0 + (lane & 15), a.N - 1), m = min(m0 + (lane & 15), a.M - 1);
-    const int64_t xo = m * a.ldx, wo = n * a.ldw;
-    f4v acc = {0.f, 0.f, 0.f, 0.f};
-    auto load = [&](const void* p, int64_t o, int k) __attribute__((always_inline)) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if constexpr (VEC) {
-            if (k < a.K) v = *(const uint4*)((const char*)p + (o + k) * (F32 ? 4 : 2));
-        } else {
-            uint32_t b[4] = {0, 0, 0, 0};
+    const int n0 = (int)(blockIdx.x % a.tn) * (16 * T);
+    const int64_t m0 = (int64_t)(blockIdx.x / a.tn) * (16 * T);
+    int64_t xo[T], wo[T];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (k + e >= a.K) continue;
-                if constexpr (F32) b[e] = ((const uint32_t*)p)[o + k + e];
-                else b[e / 2] |= (uint32_t)((const uint16_t*)p)[o + k + e] << (16 * (e & 1));
-            }
-            v = make_uint4(b[0], b[1], b[2], b[3]);
+    for (int t = 0; t < T; ++t) {
+        xo[t] = min(m0 + 16 * t + (lane & 15), a.M - 1) * a.ldx;
+        wo[t] = min(n0 + 16 * t + (lane & 15), a.N - 1) * a.ldw;
+    }
+    f4v acc[T][T];                                     // [channels][rows]
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int j = 0; j < T; ++j) acc[i][j] = f4v{0.f, 0.f, 0.f, 0.f};
+    auto load = [&](const void* p, int64_t o, int k) __attribute__((always_inline)) {
+        if constexpr (VEC) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (k < a.K) v = *(const uint4*)((const char*)p + (o + k) * (F32 ? 4 : 2));
+            return v;
+        } else {
+            return load_piece<F32>(p, o, k, a.K);
         }
-        return v;
     };
     constexpr int U = VEC ? 4 : 2;                     // pieces in flight
     for (int k0 = wave * BK; k0 < a.K; k0 += 4 * BK * U) {
-        uint4 x[U], w[U];
+        uint4 x[U][T], w[U][T];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k = k0 + u * 4 * BK + (lane >> 4) * E;
-            w[u] = load(a.w, wo, k);
-            x[u] = load(a.x, xo, k);
-        }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if constexpr (F32) {
-                const uint32_t wv[4] = {w[u].x, w[u].y, w[u].z, w[u].w}, xv[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(wv[e]), __uint_as_float(xv[e]), acc, 0, 0, 0);
-            } else {
-                acc = mfma_bf16(w[u], x[u], acc);
+            for (int t = 0; t < T; ++t) {
+                w[u][t] = load(a.w, wo[t], k);
+                x[u][t] = load(a.x, xo[t], k);
             }
         }
-    }
-    // lane l, register j: channel 4 (l / 16) + j of row l % 16
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sums[wave][j][lane] = acc[j];
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < T; ++i)
+#pragma unroll
+                for (int j = 0; j < T; ++j) {
+                    if constexpr (F32) {
+                        const uint32_t wv[4] = {w[u][i].x, w[u][i].y, w[u][i].z, w[u][i].w};
+                        const uint32_t xv[4] = {x[u][j].x, x[u][j].y, x[u][j].z, x[u][j].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(wv[e]),
+                                                                             __uint_as_float(xv[e]), acc[i][j], 0, 0, 0);
+                    } else {
+                        acc[i][j] = mfma_bf16(w[u][i], x[u][j], acc[i][j]);
+                    }
+                }
+    }
+    // lane l, register e: channel 4 (l / 16) + e of row l % 16
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int j = 0; j < T; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[wave][(i * T + j) * 4 + e][lane] = acc[i][j][e];
     __syncthreads();
     const int c = threadIdx.x & 15, row = threadIdx.x >> 4;
-    const int at = (c >> 2) * 16 + row;
-    if (n0 + c >= a.N || m0 + row >= a.M) return;
-    float z = (sums[0][c & 3][at] + sums[1][c & 3][at]) + (sums[2][c & 3][at] + sums[3][c & 3][at]);
-    if (a.bias) z += load_value<F32>(a.bias, n0 + c);
-    z = activate(z, a.act);
-    if (a.res) z += load_value<F32>(a.res, (m0 + row) * a.ldr + n0 + c);
-    if constexpr (F32) ((float*)a.y)[(m0 + row) * a.ldy + n0 + c] = z;
-    else ((uint16_t*)a.y)[(m0 + row) * a.ldy + n0 + c] = (uint16_t)bf16_pair(z, z);
+#pragma unroll
+    for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int i = 0; i < T; ++i) {
+            const int n = n0 + 16 * i + c, at = (c >> 2) * 16 + row, e = (i * T + j) * 4 + (c & 3);
+            const int64_t m = m0 + 16 * j + row;
+            if (n >= a.N || m >= a.M) continue;
+            float z[1] = {(sums[0][e][at] + sums[1][e][at]) + (sums[2][e][at] + sums[3][e][at])};
+            if (a.bias) z[0] += load_value<F32>(a.bias, n);
+            activate_all(z, a.act);
+            if (a.res) z[0] += load_value<F32>(a.res, m * a.ldr + n);
+            if constexpr (F32) ((float*)a.y)[m * a.ldy + n] = z[0];
+            else ((uint16_t*)a.y)[m * a.ldy + n] = (uint16_t)bf16_pair(z[0], z[0]);
+        }
 }
 
 namespace {
@@ -443,20 +765,38 @@ bool launch_tiles(LinearArgs& a, hipStream_t s) {
     if (tiles > 0x7FFFFFF0) return false;
     a.tiles = (int)tiles;
     a.per_xcd = (int)((tiles + 7) / 8);
+    a.packed = a.tn == 1 && a.ldy == a.N && (uintptr_t)a.y % 16 == 0;
     linear_kernel<F32, VEC, WM, WN, TM, TN><<<dim3((unsigned)a.per_xcd * 8), dim3(256), 0, s>>>(a);
+    return true;
+}
+
+bool launch_big(LinearArgs& a, hipStream_t s) {
+    a.tn = (a.N + BigShape::BN - 1) / BigShape::BN;
+    const int64_t tiles = (a.M + BigShape::BM - 1) / BigShape::BM * a.tn;
+    if (tiles > 0x7FFFFFF0) return false;
+    a.tiles = (int)tiles;
+    a.per_xcd = (int)((tiles + 7) / 8);
+    linear_big_kernel<<<dim3(256), dim3(512), 0, s>>>(a);
     return true;
 }
 
 template <bool F32, bool VEC>
 bool launch_linear(LinearArgs& a, hipStream_t s) {
-    if (a.M <= ROWS_KERNEL) {
-        a.tn = (a.N + 15) / 16;
-        const int64_t grid = (a.M + 15) / 16 * a.tn;
-        linear_rows_kernel<F32, VEC><<<dim3((unsigned)grid), dim3(256), 0, s>>>(a);
+    const int64_t n16 = (a.N + 15) / 16, n32 = (a.N + 31) / 32, few = (a.M + 63) / 64 * ((a.N + 63) / 64);
+    if (a.M <= 64 || few < FEW_TILES) {
+        const int64_t small = (a.M + 15) / 16 * n16;
+        const bool one = small <= 1024;
+        a.tn = (int)(one ? n16 : n32);
+        const dim3 grid((unsigned)(one ? small : (a.M + 31) / 32 * n32));
+        if (one) linear_rows_kernel<F32, VEC, 1><<<grid, dim3(256), 0, s>>>(a);
+        else linear_rows_kernel<F32, VEC, 2><<<grid, dim3(256), 0, s>>>(a);
         return true;
     }
     const int64_t big = ((a.M + 127) / 128) * ((a.N + 127) / 128);
-    if (a.N <= 64 && a.M >= 256 * 64) return launch_tiles<F32, VEC, 4, 1, 1, 2>(a, s);
+    if constexpr (!F32 && VEC)
+        if (a.N > 64 && big >= 1024) return launch_big(a, s);
+    // a tile of all channels, unless rows of exactly 64 can be stored as they are
+    if (a.N <= 64 && !(a.N == 64 && a.yvec) && a.M >= 256 * 64) return launch_tiles<F32, VEC, 4, 1, 1, 2>(a, s);
     if (big >= 256 && a.N > 64) return launch_tiles<F32, VEC, 2, 2, 2, 2>(a, s);
     return launch_tiles<F32, VEC, 2, 2, 1, 1>(a, s);
 }
@@ -487,8 +827,9 @@ extern "C" int sscater_linear(const sscater_linear_spec* spec, const void* x, co
     a.M = spec->rows; a.K = spec->cin; a.N = spec->cout; a.act = spec->activation;
     a.ldx = spec->x_stride; a.ldw = spec->w_stride; a.ldr = spec->residual_stride; a.ldy = spec->y_stride;
     const int per = 16 / size;
+    // 256 rows of a tile within 32-bit offsets
     const bool vec = (uintptr_t)x % 16 == 0 && (uintptr_t)weight % 16 == 0 && a.K % per == 0 && a.ldx % per == 0 &&
-                     a.ldw % per == 0;
+                     a.ldw % per == 0 && std::max(a.ldx, a.ldw) < (1 << 22);
     a.yvec = (uintptr_t)y % 16 == 0 && a.ldy % per == 0;
     a.rvec = (uintptr_t)residual % 16 == 0 && a.ldr % per == 0;
     const hipStream_t s = (hipStream_t)stream;

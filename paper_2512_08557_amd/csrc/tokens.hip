@@ -60,16 +60,12 @@ struct Piece {
 };
 
 // 16 bytes from an address that may be aligned to its elements only
-template <bool F32, bool VEC>
+template <bool VEC>
 __device__ __forceinline__ uint4 load16(const char* p) {
     if constexpr (VEC) return *(const uint4*)p;
-    if constexpr (F32) {
-        const uint32_t* u = (const uint32_t*)p;
-        return make_uint4(u[0], u[1], u[2], u[3]);
-    }
-    const uint16_t* u = (const uint16_t*)p;
-    return make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16,
-                      u[6] | (uint32_t)u[7] << 16);
+    uint4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
 }
 
 template <bool F32, int D, bool VEC>
@@ -125,7 +121,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
         const bool live = it < items;
         const int t = live ? it / heads : 0, hd = live ? it % heads : 0;
         const char* src = (const char*)a.qkv + ((int64_t)(t0 + t) * a.ld + (int64_t)hd * D) * S;
-        uint4 lo = load16<F32, VEC>(src + sub * 16), hi = load16<F32, VEC>(src + D / 2 * S + sub * 16);
+        uint4 lo = load16<VEC>(src + sub * 16), hi = load16<VEC>(src + D / 2 * S + sub * 16);
         const bool key = hd >= a.q_heads, value = hd >= a.q_heads + a.kv_heads;
         Piece<F32> x, y;
         x.unpack(lo);
@@ -140,8 +136,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
             if (weight) {
                 const float r = 1.f / sqrtf(ss * (1.f / D) + a.eps);
                 Piece<F32> wx, wy;
-                wx.unpack(load16<F32, false>((const char*)weight + sub * 16));
-                wy.unpack(load16<F32, false>((const char*)weight + D / 2 * S + sub * 16));
+                wx.unpack(load16<false>((const char*)weight + sub * 16));
+                wy.unpack(load16<false>((const char*)weight + D / 2 * S + sub * 16));
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     x.v[e] = x.v[e] * r * wx.v[e];

@@ -82,6 +82,19 @@ def test_linear_shapes(rows, cin, cout, kind):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cin,cout", [(33000, 72, 500), (32800, 200, 512), (16500, 8, 1024), (33024, 64, 512),
+                                           (20000, 24, 64), (17000, 16, 42), (16385, 33, 7)])
+def test_linear_many_rows(rows, cin, cout, kind):
+    """Several tiles for every workgroup, with ragged edges, one to four steps of K."""
+    note(f"[gpu-test] linear {rows} {cin} {cout} {kind}")
+    rng = np.random.default_rng(rows + cin + cout)
+    x, w = normal(rng, (rows, cin), KIND[kind]), normal(rng, (cout, cin), KIND[kind], cin ** -0.5)
+    b, r = normal(rng, (cout,), KIND[kind]), normal(rng, (rows, cout), KIND[kind])
+    for act, bias, res in (("gelu", b, None), ("none", None, r)):
+        close(ssc.linear(x, w, bias, activation=act, residual=res), *linear_ref(x, w, bias, act, res, kind), act)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (8, 0), (8, 8), (3, 5), (64, 0)])
 def test_linear_strides_and_alignment(kind, pad, offset):
     """Rows further apart than they are long, starting off a boundary; nothing
