@@ -25,6 +25,8 @@
 #include "tokens.h"
 
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 namespace ssc {
 
@@ -41,7 +43,8 @@ struct AttendArgs {
     int q_heads, kv_heads, group;
     int sinks, capacity, window, causal;
     int qtiles, splits;
-    float scale;           // times log2(e)
+    float scale;           // its size times log2(e)
+    uint32_t flip;         // sign bits of the queries, flipped for a negative scale
 };
 
 template <bool F32, int D, int WM>
@@ -49,19 +52,29 @@ struct AttendShape {
     static constexpr int S = F32 ? 4 : 2;
     static constexpr int RB = D * S;               // bytes of a cache row
     static constexpr int CPR = RB / 16;            // its 16-byte pieces
-    static constexpr int BN = F32 ? 32 : 64;       // keys of a tile
+    static constexpr int BN = F32 || WM == 1 ? 32 : 64;   // keys of a tile
     static constexpr int NT = BN / 32;
     static constexpr int TB = BN * RB;             // bytes of a tile
     static constexpr int WK = 4 / WM;              // groups over keys
     static constexpr int BM = 32 * WM;
     static constexpr int QN = RB / 32;             // 16-byte pieces of a lane's half of a query row
     static constexpr int ON = D / 2;               // output values of a lane
-    static constexpr int LDS = WK * 2 * TB > 4 * ON * 256 || WK == 1 ? WK * 2 * TB : 4 * ON * 256;
-    // Piece c of row r sits at piece c ^ swap: eight lanes that read one piece
-    // of neighbouring rows (K), and the four rows of a transposed read (V, two
-    // pieces each), fall on different banks.
-    static __device__ __forceinline__ int swap_k(int r) { return CPR == 4 ? (r >> 1) & 3 : r & 7; }
-    static __device__ __forceinline__ int swap_v(int r) { return F32 ? 0 : CPR == 4 ? r & 2 : (r & 3) * 2; }
+    static constexpr int GROUP = 4 * TB;           // two tiles of keys and two of values
+    static constexpr int LDS = WK * GROUP > 4 * ON * 256 || WK == 1 ? WK * GROUP : 4 * ON * 256;
+    static constexpr int WGS = LDS > 80 * 1024 || (F32 && D == 128) ? 1 : 2;   // workgroups of a compute unit
+    static constexpr int RPC = 1024 / RB;          // rows of a copy
+    static constexpr int NC = TB / 1024 / WM;      // copies of a wavefront for a tile of keys, and of values
+    // Piece c of row r sits at piece c ^ swap: sixteen lanes that read one piece
+    // of neighbouring rows (K), and the four rows of a transposed read by 32 lanes
+    // (V, four pieces each), fall on different banks of the 64.  fp32 values are
+    // read by 32 lanes from one row and by 32 from the row four further on.
+    static __device__ __forceinline__ int swap_k(int r) {
+        return CPR == 4 ? (r >> 2) & 3 : CPR == 8 ? (r >> 1) & 7 : r & 15;
+    }
+    static __device__ __forceinline__ int swap_v(int r) {
+        if (F32) return CPR == 8 ? 0 : (r & 4) * 2;
+        return CPR == 4 ? 0 : CPR == 8 ? (r & 2) * 2 : (r & 3) * 4;
+    }
 };
 
 // What a tile of rows reaches.
@@ -81,11 +94,11 @@ __device__ __forceinline__ int slot_of(const AttendArgs& a, const Reach& r, int 
 }
 
 template <bool F32, int D, int WM>
-__global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_kernel(AttendArgs a) {
     using C = AttendShape<F32, D, WM>;
     __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
     __shared__ float ml[4][32][2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wk = wave / WM;
     const int h = lane >> 5, col = lane & 31;
     int id = blockIdx.x;
@@ -118,7 +131,13 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
     {
         const char* p = (const char*)a.q + qrow * C::RB + h * 16;
 #pragma unroll
-        for (int s = 0; s < C::QN; ++s) qf[s] = *(const uint4*)(p + s * 32);
+        for (int s = 0; s < C::QN; ++s) {
+            qf[s] = *(const uint4*)(p + s * 32);
+            qf[s].x ^= a.flip;
+            qf[s].y ^= a.flip;
+            qf[s].z ^= a.flip;
+            qf[s].w ^= a.flip;
+        }
     }
     f16v o[D / 32];
 #pragma unroll
@@ -131,89 +150,104 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
     const int64_t head = ((int64_t)b * a.kv_heads + kvh) * a.capacity * C::RB;
     const char* kg = (const char*)a.k + head;
     const char* vg = (const char*)a.v + head;
-    lds_char* kl = (lds_char*)lds + wk * 2 * C::TB;
-    lds_char* vl = kl + C::TB;
+    lds_char* own = (lds_char*)lds + wk * C::GROUP;
     // rows of the wavefront that see least, for the choice of the masked form
     const int wl_first = __builtin_amdgcn_readfirstlane(last);
     const int wf_last = __builtin_amdgcn_readlane(from, 31);
-    const int wl_last = __builtin_amdgcn_readlane(last, 31), wf_first = __builtin_amdgcn_readfirstlane(from);
 
-    for (int t0 = tb; t0 < te; t0 += C::WK) {
-        const int u0 = (t0 + wk) * C::BN;
-        const bool live = t0 + wk < te;
-        __syncthreads();
-        if (live) {
-            constexpr int RPC = 1024 / C::RB;      // rows of a copy
+    // Copies of a tile: a lane's place within it is always the same, so for keys
+    // that lie one behind the other only the uniform base moves.
+    const int row0 = wm * C::RPC + lane / C::CPR, pc = lane % C::CPR;
+    // all copies of tile t's keys or values
+    auto copy = [&](int t, const char* from, auto value, lds_char* to) __attribute__((always_inline)) {
+        constexpr bool V = decltype(value)::value;
+        const int u = t * C::BN, ring = a.capacity - a.sinks;
+        int x = reach.base + (u - a.sinks);
+        if (x >= ring) x -= ring;
+        const bool sink = u + C::BN <= a.sinks;
+        if (u + C::BN <= reach.total && (sink || (u >= a.sinks && x + C::BN <= ring))) {
+            from += (int64_t)(sink ? u : a.sinks + x) * C::RB;
 #pragma unroll
-            for (int i = 0; i < C::TB / 1024 / WM; ++i) {
-                const int c = i * WM + wm;
-                const int r = c * RPC + lane / C::CPR, pc = lane % C::CPR;
-                const int64_t at = (int64_t)slot_of(a, reach, min(u0 + r, reach.total - 1)) * C::RB;
-                copy16(kg + at + (pc ^ C::swap_k(r)) * 16, kl + c * 1024);
-                copy16(vg + at + (pc ^ C::swap_v(r)) * 16, vl + c * 1024);
+            for (int j = 0; j < C::NC; ++j) {
+                const int r = j * (WM * C::RPC) + row0;
+                copy16(from + (uint32_t)(r * C::RB + (pc ^ (V ? C::swap_v(r) : C::swap_k(r))) * 16),
+                       to + (j * WM + wm) * 1024);
+            }
+        } else {
+            // the ring's end, the sinks' end or the last key cuts it
+#pragma unroll 1
+            for (int j = 0; j < C::NC; ++j) {
+                const int r = j * (WM * C::RPC) + row0;
+                const int64_t at = (int64_t)slot_of(a, reach, min(u + r, reach.total - 1)) * C::RB;
+                copy16(from + at + (pc ^ (V ? C::swap_v(r) : C::swap_k(r))) * 16, to + (j * WM + wm) * 1024);
             }
         }
+    };
+    // the group's tiles are tb + wk, tb + wk + WK, ...; groups that share a workgroup go round as often as the first
+    const int mine = te - tb > wk ? (te - tb - wk + C::WK - 1) / C::WK : 0;
+    const int rounds = WM == 1 ? mine : (te - tb + C::WK - 1) / C::WK;
+    auto tile_of = [&](int j) __attribute__((always_inline)) { return tb + wk + j * C::WK; };
+    auto meet = [&]() __attribute__((always_inline)) {
         wait_vm<0>();
-        __syncthreads();
-        if (!live || u0 > wl_last || (u0 + C::BN <= wf_first && u0 >= a.sinks)) continue;
-        f16v s[C::NT];
+        // a wavefront with tiles of its own waits for no one
+        if (WM > 1) lds_barrier();
+        else asm volatile("" ::: "memory");
+    };
+    lds_char* const kbuf = own;
+    lds_char* const vbuf = own + 2 * C::TB;
+
+    constexpr int STEPS = C::NT * C::QN;               // of the product with the keys
+    auto key_step = [&](f16v (&s)[C::NT], int i, const uint4 kf) __attribute__((always_inline)) {
+        const int t = i / C::QN, c = i % C::QN;
+        if constexpr (F32) {
+            const uint32_t kv[4] = {kf.x, kf.y, kf.z, kf.w}, qv[4] = {qf[c].x, qf[c].y, qf[c].z, qf[c].w};
 #pragma unroll
-        for (int t = 0; t < C::NT; ++t) {
-            s[t] = f16v{};
-            const int r = 32 * t + col;
-#pragma unroll
-            for (int i = 0; i < C::QN; ++i) {
-                const uint4 kf = lds16(kl + r * C::RB + ((2 * i + h) ^ C::swap_k(r)) * 16);
-                if constexpr (F32) {
-                    const uint32_t kv[4] = {kf.x, kf.y, kf.z, kf.w}, qv[4] = {qf[i].x, qf[i].y, qf[i].z, qf[i].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kv[e]), __uint_as_float(qv[e]), s[t],
-                                                                    0, 0, 0);
-                } else {
-                    bf8v A, B;
-                    __builtin_memcpy(&A, &kf, 16);
-                    __builtin_memcpy(&B, &qf[i], 16);
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, B, s[t], 0, 0, 0);
-                }
-            }
+            for (int e = 0; e < 4; ++e)
+                s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kv[e]), __uint_as_float(qv[e]), s[t], 0, 0, 0);
+        } else {
+            bf8v A, B;
+            __builtin_memcpy(&A, &kf, 16);
+            __builtin_memcpy(&B, &qf[c], 16);
+            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, B, s[t], 0, 0, 0);
         }
-        const bool masked = u0 + C::BN - 1 > wl_first || (u0 < wf_last && u0 + C::BN > a.sinks);
-        float mx = -INFINITY;
+    };
+    auto key_load = [&](const lds_char* kl, int i) __attribute__((always_inline)) {
+        const int r = 32 * (i / C::QN) + col;
+        return lds16(kl + r * C::RB + ((2 * (i % C::QN) + h) ^ C::swap_k(r)) * 16);
+    };
+    auto clear = [&](f16v (&s)[C::NT]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int t = 0; t < C::NT; ++t)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                float x = s[t][j] * a.scale;
-                if (masked) {
-                    const int u = u0 + 32 * t + 8 * (j >> 2) + 4 * h + (j & 3);
-                    x = u <= last && (u >= from || u < a.sinks) ? x : -INFINITY;
-                }
-                s[t][j] = x;
-                mx = fmaxf(mx, x);
-            }
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mn = fmaxf(m, mx), ms = mn == -INFINITY ? 0.f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(m - ms);
-        m = mn;
-        float sum = 0.f;
-#pragma unroll
-        for (int t = 0; t < C::NT; ++t)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                s[t][j] = __builtin_amdgcn_exp2f(s[t][j] - ms);
-                sum += s[t][j];
-            }
-        l = l * alpha + sum;
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[t][j] *= alpha;
-        bool plain = true;
+        for (int t = 0; t < C::NT; ++t) s[t] = f16v{};
+    };
+
+    bool again = false;
+    // Round j: the softmax of tile j's scores s beside the products that give tile
+    // j + 1's, in n (a wavefront's vector instructions run while its matrix
+    // instructions do, if they are next to each other), then the product with the
+    // values.  P: j & 1.
+    auto round = [&](int j, auto parity, f16v (&s)[C::NT], f16v (&n)[C::NT]) __attribute__((always_inline)) {
+        constexpr int P = decltype(parity)::value;
+        meet();
+        if (j + 2 < mine) copy(tile_of(j + 2), kg, std::false_type{}, kbuf + P * C::TB);
+        if (j + 1 < mine) copy(tile_of(j + 1), vg, std::true_type{}, vbuf + (1 - P) * C::TB);
+        const lds_char* kl = kbuf + (1 - P) * C::TB;
+        const lds_char* vl = vbuf + P * C::TB;
+        const int u0 = tile_of(j) * C::BN;
+        clear(n);
+        // a tile that the wavefront does not see at all goes the same way (skipping it cost registers, and it spilled)
+        const bool masked = j >= mine || u0 + C::BN - 1 > wl_first || (u0 < wf_last && u0 + C::BN > a.sinks);
         if (masked) {
-            // A masked key's probability is zero, but its values may be
-            // infinite or NaN: those tiles go key by key, past the masked ones.
+#pragma unroll
+            for (int t = 0; t < C::NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int u = u0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
+                    s[t][e] = j < mine && u <= last && (u >= from || u < a.sinks) ? s[t][e] : -INFINITY;
+                }
+            // A masked key's probability is zero, but its values may be infinite
+            // or NaN, and the matrix product would carry those to every row.
             uint32_t big = 0;
+#pragma unroll 2
             for (int i = lane; i < C::TB / 16; i += 64) {
                 const uint4 v = lds16(vl + i * 16);
                 for (uint32_t w : {v.x, v.y, v.z, v.w}) {
@@ -221,50 +255,77 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
                     else big |= ((w & 0x7F80u) == 0x7F80u) | ((w & 0x7F800000u) == 0x7F800000u);
                 }
             }
-            plain = __ballot(big != 0) == 0;
+            again |= __ballot(big != 0) != 0;
         }
-        if (!plain) {
-#pragma unroll 1
-            for (int kk = 0; kk < C::BN; ++kk) {
-                float p = 0.f;
+        // (past the last tile these are products of what the buffer holds; nobody reads them)
+        constexpr int FIRST = STEPS / 4;
+        uint4 kf[2];
+        kf[0] = key_load(kl, 0);
 #pragma unroll
-                for (int e = 0; e < 16 * C::NT; ++e) {
-                    const int key = 32 * (e >> 4) + 8 * ((e >> 2) & 3) + (e & 3);
-                    if (key == (kk & ~4)) p = s[e >> 4][e & 15];
-                }
-                p = __shfl(p, col + 8 * (kk & 4));
-                const int u = u0 + kk;
-                const bool sees = u <= last && (u >= from || u < a.sinks);
+        for (int i = 0; i < FIRST; ++i) {
+            kf[(i + 1) & 1] = key_load(kl, i + 1);
+            key_step(n, i, kf[i & 1]);
+        }
+        float mx = s[0][0];
 #pragma unroll
-                for (int e = 0; e < C::ON; ++e) {
-                    const int d = 32 * (e >> 4) + 8 * ((e >> 2) & 3) + 4 * h + (e & 3);
-                    const lds_char* at = vl + kk * C::RB + ((d * C::S / 16) ^ C::swap_v(kk)) * 16 + d * C::S % 16;
-                    float v;
-                    if constexpr (F32) v = *(const __attribute__((address_space(3))) float*)at;
-                    else v = __uint_as_float((uint32_t)*(const __attribute__((address_space(3))) uint16_t*)at << 16);
-                    if (sees) o[e >> 4][e & 15] = fmaf(p, v, o[e >> 4][e & 15]);
+        for (int t = 0; t < C::NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[t][e]);
+        {
+            const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])) * a.scale;
+        }
+        // m is the reference of the row's exponents: a probability may be up to 2^8
+        // before it moves, so that the sums are hardly ever scaled again
+        if (__ballot(mx > m + 8.f) != 0) {
+            const float mn = fmaxf(m, mx);
+            const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.f : mn));
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+        }
+        const float ms = m == -INFINITY ? 0.f : m;
+        uint4 pf[C::NT * 2];                           // bf16: eight probabilities each
+        constexpr int ALL = 16 * C::NT, LEFT = STEPS - FIRST;
+#pragma unroll
+        for (int i = 0; i < LEFT; ++i) {
+            if (FIRST + i + 1 < STEPS) kf[(FIRST + i + 1) & 1] = key_load(kl, FIRST + i + 1);
+            key_step(n, FIRST + i, kf[(FIRST + i) & 1]);
+#pragma unroll
+            for (int e = i * ALL / LEFT; e < (i + 1) * ALL / LEFT; ++e) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], a.scale, -ms));
+                s[e >> 4][e & 15] = x;
+                l += x;
+                if (!F32 && (e & 1)) {
+                    const uint32_t w = bf16_pair(s[e >> 4][(e & 15) - 1], x);
+                    uint4& f = pf[e >> 3];
+                    if ((e & 7) == 1) f.x = w;
+                    else if ((e & 7) == 3) f.y = w;
+                    else if ((e & 7) == 5) f.z = w;
+                    else f.w = w;
                 }
             }
-        } else if constexpr (F32) {
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (F32) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int key = 8 * (j >> 2) + 4 * h + (j & 3);
+            for (int e = 0; e < 16; ++e) {
+                const int key = 8 * (e >> 2) + 4 * h + (e & 3);
 #pragma unroll
                 for (int t = 0; t < D / 32; ++t) {
-                    const float v = *(const __attribute__((address_space(3))) float*)(vl + key * C::RB + (32 * t + col) * 4);
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[0][j], o[t], 0, 0, 0);
+                    const int at = key * C::RB + (((8 * t + col / 4) ^ C::swap_v(key)) * 4 + col % 4) * 4;
+                    const float v = *(const __attribute__((address_space(3))) float*)(vl + at);
+                    o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[0][e], o[t], 0, 0, 0);
                 }
             }
         } else {
 #pragma unroll
             for (int ks = 0; ks < C::BN / 16; ++ks) {
-                uint4 pf;
-                const f16v& sv = s[ks / 2];
-                const int j = 8 * (ks & 1);
-                pf = make_uint4(bf16_pair(sv[j], sv[j + 1]), bf16_pair(sv[j + 2], sv[j + 3]),
-                                bf16_pair(sv[j + 4], sv[j + 5]), bf16_pair(sv[j + 6], sv[j + 7]));
                 bf8v B;
-                __builtin_memcpy(&B, &pf, 16);
+                __builtin_memcpy(&B, &pf[ks], 16);
                 const int i = lane & 15, key = 16 * ks + 4 * h + (i >> 2);
                 // rows key and key + 8 have the same swap
                 const lds_char* at = vl + key * C::RB + 8 * (i & 1);
@@ -281,6 +342,64 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
                 }
             }
         }
+    };
+
+    f16v sa[C::NT], sb[C::NT];
+    clear(sa);
+    if (mine > 0) copy(tile_of(0), kg, std::false_type{}, kbuf);
+    meet();
+    if (mine > 0) {
+        copy(tile_of(0), vg, std::true_type{}, vbuf);
+        if (mine > 1) copy(tile_of(1), kg, std::false_type{}, kbuf + C::TB);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) key_step(sa, i, key_load(kbuf, i));
+    }
+    for (int j = 0; j < rounds; j += 2) {
+        round(j, std::integral_constant<int, 0>{}, sa, sb);
+        if (j + 1 < rounds) round(j + 1, std::integral_constant<int, 1>{}, sb, sa);
+    }
+    if (again) {
+        // Keys one by one, each only for the rows that see it: the wavefront's
+        // sums formed again from the cache.
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) o[t] = f16v{};
+        const char* qr = (const char*)a.q + qrow * C::RB;
+#pragma unroll 1
+        for (int u = tb * C::BN; u < min(te * C::BN, reach.total); ++u) {
+            if ((u / C::BN - tb) % C::WK != wk || !(u <= last && (u >= from || u < a.sinks))) continue;
+            const int64_t at = (int64_t)slot_of(a, reach, u) * C::RB;
+            float x = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < C::CPR; ++c) {
+                uint4 qv = *(const uint4*)(qr + c * 16), kv = *(const uint4*)(kg + at + c * 16);
+                const uint32_t qw[4] = {qv.x ^ a.flip, qv.y ^ a.flip, qv.z ^ a.flip, qv.w ^ a.flip};
+                const uint32_t kw[4] = {kv.x, kv.y, kv.z, kv.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (F32) {
+                        x = fmaf(__uint_as_float(qw[e]), __uint_as_float(kw[e]), x);
+                    } else {
+                        x = fmaf(__uint_as_float(qw[e] << 16), __uint_as_float(kw[e] << 16), x);
+                        x = fmaf(__uint_as_float(qw[e] & 0xFFFF0000u), __uint_as_float(kw[e] & 0xFFFF0000u), x);
+                    }
+                }
+            }
+            x *= a.scale;
+            const float mn = fmaxf(m, x), ms = mn == -INFINITY ? 0.f : mn;
+            const float alpha = __builtin_amdgcn_exp2f(m - ms), p = __builtin_amdgcn_exp2f(x - ms);
+            m = mn;
+            l = fmaf(l, alpha, p);
+            const char* vr = vg + at;
+#pragma unroll
+            for (int e = 0; e < C::ON; ++e) {
+                const int d = 32 * (e >> 4) + 8 * ((e >> 2) & 3) + 4 * h + (e & 3);
+                const float v = F32 ? ((const float*)vr)[d] : __uint_as_float((uint32_t)((const uint16_t*)vr)[d] << 16);
+                o[e >> 4][e & 15] = fmaf(p, v, o[e >> 4][e & 15] * alpha);
+            }
+        }
+        if (h == 1) l = 0.f;                           // both lanes of a row have all of its sum
     }
     l += __shfl_xor(l, 32);
 
@@ -292,7 +411,7 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(AttendArgs a) {
             ml[wave][col][0] = m;
             ml[wave][col][1] = l;
         }
-        __syncthreads();
+        __syncthreads();               // all tiles have been read, too
         float* x = (float*)lds;
 #pragma unroll
         for (int e = 0; e < C::ON; ++e) x[(wave * C::ON + e) * 64 + lane] = o[e >> 4][e & 15];
@@ -378,11 +497,12 @@ bool attend_cut(const sscater_attend_spec* s, const sscater_token_cache* c, cons
     if (r->tokens > 0 && c->capacity - c->sinks < reach) return false;
     const int64_t rows = (int64_t)r->max_new * (s->q_heads / c->kv_heads);
     if (rows > (1 << 30) || (int64_t)r->tokens * s->q_heads > (int64_t(1) << 40)) return false;
-    cut->wm = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    // fp32 heads of 128 values: two tiles of keys and of values for each of four wavefronts would not fit
+    cut->wm = rows <= 32 && !(c->dtype == SSCATER_F32 && c->head_dim == 128) ? 1 : rows <= 64 ? 2 : 4;
     cut->qtiles = (int)((rows + 32 * cut->wm - 1) / (32 * cut->wm));
     const int64_t base = (int64_t)cut->qtiles * c->kv_heads * c->batch;
     const int64_t keys = reach + c->sinks;
-    const int bn = (c->dtype == SSCATER_F32 ? 32 : 64) * (4 / cut->wm);
+    const int bn = (c->dtype == SSCATER_F32 || cut->wm == 1 ? 32 : 64) * (4 / cut->wm);
     cut->splits = 1;
     if (base > 0 && base < 256)
         cut->splits = (int)std::max((int64_t)1, std::min((512 + base - 1) / base, (keys + 2 * bn - 1) / (2 * bn)));
@@ -398,9 +518,11 @@ size_t attend_bytes(const AttendCut& cut, const sscater_attend_spec* s, const ss
 template <bool F32, int D>
 void launch_attend(const AttendArgs& a, const AttendCut& cut, hipStream_t s) {
     const dim3 grid((unsigned)cut.grid), block(256);
-    if (cut.wm == 1) attend_kernel<F32, D, 1><<<grid, block, 0, s>>>(a);
-    else if (cut.wm == 2) attend_kernel<F32, D, 2><<<grid, block, 0, s>>>(a);
-    else attend_kernel<F32, D, 4><<<grid, block, 0, s>>>(a);
+    if constexpr (!(F32 && D == 128)) {
+        if (cut.wm == 1) attend_kernel<F32, D, 1><<<grid, block, 0, s>>>(a);
+    }
+    if (cut.wm == 2) attend_kernel<F32, D, 2><<<grid, block, 0, s>>>(a);
+    if (cut.wm == 4) attend_kernel<F32, D, 4><<<grid, block, 0, s>>>(a);
     if (cut.splits > 1) {
         const int64_t rows = (int64_t)a.rows.tokens * a.q_heads;
         join_kernel<F32, D><<<dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), block, 0, s>>>(a.part, a.out, rows,
@@ -446,7 +568,8 @@ int sscater_tokens_attend(const sscater_attend_spec* spec, const sscater_token_c
     a.q_heads = spec->q_heads; a.kv_heads = cache->kv_heads; a.group = spec->q_heads / cache->kv_heads;
     a.sinks = cache->sinks; a.capacity = cache->capacity; a.window = spec->window; a.causal = spec->causal;
     a.qtiles = cut.qtiles; a.splits = cut.splits;
-    a.scale = spec->scale * 1.4426950408889634f;
+    a.scale = std::max(std::fabs(spec->scale) * 1.4426950408889634f, 1e-30f);   // times -inf it stays that
+    a.flip = spec->scale < 0.f ? cache->dtype == SSCATER_F32 ? 0x80000000u : 0x80008000u : 0u;
     if (cache->dtype == SSCATER_F32) launch_attend<true>(a, cut, cache->head_dim, (hipStream_t)stream);
     else launch_attend<false>(a, cut, cache->head_dim, (hipStream_t)stream);
     const hipError_t e = hipGetLastError();
