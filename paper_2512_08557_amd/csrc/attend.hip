@@ -118,7 +118,10 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     reach.n_sinks = (int)min((int64_t)a.sinks, reach.lo);
     reach.total = (int)min((int64_t)a.capacity,
                            reach.n_sinks + (a.causal ? past + i1 + 1 : past + n) - reach.lo);
-    reach.base = (int)((max(reach.lo, (int64_t)a.sinks) - a.sinks) % (a.capacity - a.sinks));
+    // (a 64-bit remainder takes half a microsecond; streams are that long only after hours)
+    const int64_t beyond = max(reach.lo, (int64_t)a.sinks) - a.sinks;
+    const uint32_t ring = a.capacity - a.sinks;
+    reach.base = beyond >> 32 == 0 ? (int)((uint32_t)beyond % ring) : (int)(beyond % ring);
     const int row = min(tile * C::BM + wm * 32 + col, nr - 1);
     const int tok = row / a.group;
     const int64_t qrow = ((int64_t)(first + tok) * a.q_heads + kvh * a.group + row % a.group);
@@ -259,13 +262,16 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         }
         // (past the last tile these are products of what the buffer holds; nobody reads them)
         constexpr int FIRST = STEPS / 4;
-        uint4 kf[2];
-        kf[0] = key_load(kl, 0);
+        constexpr int KA = STEPS < 4 ? 2 : 4;          // operands under way: LDS answers after about four products
+        uint4 kf[KA];
 #pragma unroll
-        for (int i = 0; i < FIRST; ++i) {
-            kf[(i + 1) & 1] = key_load(kl, i + 1);
-            key_step(n, i, kf[i & 1]);
-        }
+        for (int i = 0; i < KA - 1; ++i) kf[i] = key_load(kl, i);
+        auto key_next = [&](int i) __attribute__((always_inline)) {
+            if (i + KA - 1 < STEPS) kf[(i + KA - 1) % KA] = key_load(kl, i + KA - 1);
+            key_step(n, i, kf[i % KA]);
+        };
+#pragma unroll
+        for (int i = 0; i < FIRST; ++i) key_next(i);
         float mx = s[0][0];
 #pragma unroll
         for (int t = 0; t < C::NT; ++t)
@@ -278,6 +284,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         // m is the reference of the row's exponents: a probability may be up to 2^8
         // before it moves, so that the sums are hardly ever scaled again
         if (__ballot(mx > m + 8.f) != 0) {
+            asm volatile("");                          // a branch: the compiler would scale by 1 instead
             const float mn = fmaxf(m, mx);
             const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.f : mn));
             m = mn;
@@ -289,11 +296,37 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         }
         const float ms = m == -INFINITY ? 0.f : m;
         uint4 pf[C::NT * 2];                           // bf16: eight probabilities each
+        // the values of 16 keys (bf16) or of two (fp32), all of a head
+        constexpr int VS = F32 ? 16 : C::BN / 16, VA = F32 ? 4 : 2;
+        uint4 vf[VA][D / 32];
+        auto value_load = [&](int ks) __attribute__((always_inline)) {
+            if constexpr (F32) {
+                const int key = 8 * (ks >> 2) + 4 * h + (ks & 3);
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) {
+                    const int at = key * C::RB + (((8 * t + col / 4) ^ C::swap_v(key)) * 4 + col % 4) * 4;
+                    vf[ks % VA][t].x = *(const __attribute__((address_space(3))) uint32_t*)(vl + at);
+                }
+            } else {
+                const int i = lane & 15, key = 16 * ks + 4 * h + (i >> 2);
+                // rows key and key + 8 have the same swap
+                const lds_char* at = vl + key * C::RB + 8 * (i & 1);
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) {
+                    const int c = (4 * t + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1)) ^ C::swap_v(key);
+                    typedef __attribute__((address_space(3))) s4v lds_s4v;
+                    const s4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + c * 16));
+                    const s4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + 8 * C::RB + c * 16));
+                    __builtin_memcpy(&vf[ks % VA][t], &v0, 8);
+                    __builtin_memcpy((char*)&vf[ks % VA][t] + 8, &v1, 8);
+                }
+            }
+        };
         constexpr int ALL = 16 * C::NT, LEFT = STEPS - FIRST;
 #pragma unroll
         for (int i = 0; i < LEFT; ++i) {
-            if (FIRST + i + 1 < STEPS) kf[(FIRST + i + 1) & 1] = key_load(kl, FIRST + i + 1);
-            key_step(n, FIRST + i, kf[(FIRST + i) & 1]);
+            if (i == LEFT - (LEFT + 3) / 4) value_load(0);
+            key_next(FIRST + i);
 #pragma unroll
             for (int e = i * ALL / LEFT; e < (i + 1) * ALL / LEFT; ++e) {
                 const float x = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], a.scale, -ms));
@@ -310,37 +343,24 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (F32) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int key = 8 * (e >> 2) + 4 * h + (e & 3);
+        for (int d = 1; d < VA - 1; ++d) value_load(d);
 #pragma unroll
-                for (int t = 0; t < D / 32; ++t) {
-                    const int at = key * C::RB + (((8 * t + col / 4) ^ C::swap_v(key)) * 4 + col % 4) * 4;
-                    const float v = *(const __attribute__((address_space(3))) float*)(vl + at);
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[0][e], o[t], 0, 0, 0);
-                }
-            }
-        } else {
+        for (int ks = 0; ks < VS; ++ks) {
+            if (ks + VA - 1 < VS) value_load(ks + VA - 1);
 #pragma unroll
-            for (int ks = 0; ks < C::BN / 16; ++ks) {
-                bf8v B;
-                __builtin_memcpy(&B, &pf[ks], 16);
-                const int i = lane & 15, key = 16 * ks + 4 * h + (i >> 2);
-                // rows key and key + 8 have the same swap
-                const lds_char* at = vl + key * C::RB + 8 * (i & 1);
-#pragma unroll
-                for (int t = 0; t < D / 32; ++t) {
-                    const int c = (4 * t + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1)) ^ C::swap_v(key);
-                    typedef __attribute__((address_space(3))) s4v lds_s4v;
-                    const s4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + c * 16));
-                    const s4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + 8 * C::RB + c * 16));
-                    bf8v A;
-                    __builtin_memcpy(&A, &v0, 8);
-                    __builtin_memcpy((char*)&A + 8, &v1, 8);
+            for (int t = 0; t < D / 32; ++t) {
+                const uint4 v = vf[ks % VA][t];
+                if constexpr (F32) {
+                    o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v.x), s[0][ks], o[t], 0, 0, 0);
+                } else {
+                    bf8v A, B;
+                    __builtin_memcpy(&A, &v, 16);
+                    __builtin_memcpy(&B, &pf[ks], 16);
                     o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, B, o[t], 0, 0, 0);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -455,29 +475,53 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         *(float2*)(a.part + a.splits * out_rows * D + (split * out_rows + qrow) * 2) = make_float2(m, l);
 }
 
-// The splits' sums of one row, joined: D / 4 lanes a row.
+constexpr int MAX_SPLITS = 64;
+
+// The splits' sums of one row, joined by a wavefront: lane s forms split s's
+// weight, then groups of D / 4 lanes take every (256 / D)th split's sums, four of
+// them under way, and are added up.  (Splits one after the other in one group of
+// lanes: 9.3 us for 17 of them, against 7.7 for the attention itself.)
 template <bool F32, int D>
 __global__ __launch_bounds__(256) void join_kernel(const float* part, void* out, int64_t rows, int splits) {
-    const int64_t row = (int64_t)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+    constexpr int G = 256 / D;                         // groups
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= rows) return;
-    const int d = threadIdx.x % (D / 4) * 4;
-    const float* ml = part + splits * rows * D + row * 2;
-    float big = -INFINITY;
-    for (int s = 0; s < splits; ++s) big = fmaxf(big, ml[s * rows * 2]);
-    const float ms = big == -INFINITY ? 0.f : big;
-    float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) {
-        const float f = __builtin_amdgcn_exp2f(ml[s * rows * 2] - ms);
-        const float4 p = *(const float4*)(part + (s * rows + row) * D + d);
-        l = fmaf(f, ml[s * rows * 2 + 1], l);
-        v[0] = fmaf(f, p.x, v[0]);
-        v[1] = fmaf(f, p.y, v[1]);
-        v[2] = fmaf(f, p.z, v[2]);
-        v[3] = fmaf(f, p.w, v[3]);
+    const int lane = threadIdx.x & 63, d = lane % (D / 4) * 4, g = lane / (D / 4);
+    const float* from = part + row * D + d;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < splits) ml = *(const float2*)(part + splits * rows * D + (lane * rows + row) * 2);
+    float big = ml.x;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) big = fmaxf(big, __shfl_xor(big, i));
+    const float f = __builtin_amdgcn_exp2f(ml.x - (big == -INFINITY ? 0.f : big));
+    float l = f * ml.y;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) l += __shfl_xor(l, i);
+    f4v v = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < splits; s0 += 4 * G) {
+        f4v p[4];
+        float w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int s = s0 + i * G + g;
+            p[i] = s < splits ? *(const f4v*)(from + s * rows * D) : f4v{0.f, 0.f, 0.f, 0.f};
+            w[i] = __shfl(f, min(s, MAX_SPLITS - 1));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(w[i], p[i][e], v[e]);
     }
     const float r = 1.f / l;
-    if constexpr (F32) *(float4*)((float*)out + row * D + d) = make_float4(v[0] * r, v[1] * r, v[2] * r, v[3] * r);
-    else *(uint2*)((uint16_t*)out + row * D + d) = make_uint2(bf16_pair(v[0] * r, v[1] * r), bf16_pair(v[2] * r, v[3] * r));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int i = D / 4; i < 64; i <<= 1) v[e] += __shfl_xor(v[e], i);
+        v[e] *= r;
+    }
+    if (g != 0) return;
+    if constexpr (F32) *(f4v*)((float*)out + row * D + d) = v;
+    else *(uint2*)((uint16_t*)out + row * D + d) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
 }
 
 namespace {
@@ -505,7 +549,7 @@ bool attend_cut(const sscater_attend_spec* s, const sscater_token_cache* c, cons
     const int bn = (c->dtype == SSCATER_F32 || cut->wm == 1 ? 32 : 64) * (4 / cut->wm);
     cut->splits = 1;
     if (base > 0 && base < 256)
-        cut->splits = (int)std::max((int64_t)1, std::min((512 + base - 1) / base, (keys + 2 * bn - 1) / (2 * bn)));
+        cut->splits = (int)std::max((int64_t)1, std::min({(512 + base - 1) / base, (keys + 2 * bn - 1) / (2 * bn), (int64_t)MAX_SPLITS}));
     cut->grid = base * cut->splits;
     return cut->grid <= 0x7FFFFFFF;
 }
@@ -525,8 +569,7 @@ void launch_attend(const AttendArgs& a, const AttendCut& cut, hipStream_t s) {
     if (cut.wm == 4) attend_kernel<F32, D, 4><<<grid, block, 0, s>>>(a);
     if (cut.splits > 1) {
         const int64_t rows = (int64_t)a.rows.tokens * a.q_heads;
-        join_kernel<F32, D><<<dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), block, 0, s>>>(a.part, a.out, rows,
-                                                                                                  cut.splits);
+        join_kernel<F32, D><<<dim3((unsigned)((rows + 3) / 4)), block, 0, s>>>(a.part, a.out, rows, cut.splits);
     }
 }
 

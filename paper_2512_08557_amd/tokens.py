@@ -18,13 +18,17 @@ from .engine import BF16, F32, SscaterError, _check, lib
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
-def _kind(t) -> int:
-    import torch
-    if t.dtype is torch.float32:
-        return F32
-    if t.dtype is torch.bfloat16:
-        return BF16
-    raise ValueError(f"float32 or bfloat16 tensors, not {t.dtype}")
+torch = _device = _stream = None
+_KINDS: dict = {}
+
+
+def _bind():
+    """torch, at the first call (as in Engine), and its current device and
+    stream as plain numbers: the objects around them cost more than a launch."""
+    global torch, _device, _stream
+    import torch as t
+    torch, _device, _stream = t, t._C._cuda_getDevice, t._C._cuda_getCurrentRawStream
+    _KINDS.update({t.float32: F32, t.bfloat16: BF16})
 
 
 def _require(t, name: str, dtype, index: int, shape=None):
@@ -49,11 +53,9 @@ def _dense(t, name: str, dtype, index: int, shape):
 def _launch(fn, where: str, index: int, stream, tensors, *args) -> None:
     """One library call on device `index`, on torch's current stream; another
     stream first waits for that one, and the call's tensors are recorded there
-    (as in Engine).  The current stream's handle is asked for as a number: the
-    object around it costs more than the rest of the call."""
-    import torch
-    if stream is None and torch._C._cuda_getDevice() == index:
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    (as in Engine)."""
+    if stream is None and _device() == index:
+        rc = fn(*args, _stream(index))
     else:
         with torch.cuda.device(index):
             cur = torch.cuda.current_stream()
@@ -103,7 +105,12 @@ def linear(x, weight, bias=None, activation: Optional[str] = None, residual=None
     act = ACTIVATIONS.get(activation, -1)
     if act < 0:
         raise ValueError(f"activation must be one of {sorted(k for k in ACTIVATIONS if k)}")
-    kind, dtype = _kind(x), x.dtype
+    if torch is None:
+        _bind()
+    dtype = x.dtype
+    kind = _KINDS.get(dtype, -1)
+    if kind < 0:
+        raise ValueError(f"float32 or bfloat16 tensors, not {dtype}")
     if weight.dim() != 2:
         raise ValueError("weight must be [cout, cin]")
     cout, cin = weight.shape
@@ -140,7 +147,8 @@ class Rotary:
 
     def __init__(self, inv_freq, sections: Sequence[int], interleaved: bool = False, base: float = 10000.0,
                  device="cuda"):
-        import torch
+        if torch is None:
+            _bind()
         self.sections = tuple(int(n) for n in sections)
         if not 1 <= len(self.sections) <= 3 or any(n < 0 for n in self.sections):
             raise ValueError("one to three axes")
@@ -169,7 +177,8 @@ class TokenCache:
 
     def __init__(self, batch: int, kv_heads: int, head_dim: int, capacity: int, sinks: int = 0, dtype: str = "f32",
                  k=None, v=None, device="cuda"):
-        import torch
+        if torch is None:
+            _bind()
         if dtype not in ("f32", "bf16"):
             raise ValueError("dtype must be f32 or bf16")
         if batch < 1 or kv_heads < 1 or head_dim not in (32, 64, 128):
@@ -187,25 +196,26 @@ class TokenCache:
         self.index = k.get_device()
         for name, t in (("k", k), ("v", v)):
             _dense(t, name, kind, self.index, shape)
-        self.k, self.v, self.kind = k, v, kind
-        self.past = torch.zeros(self.batch, dtype=torch.int64, device=k.device)
+        self._k, self._v, self.kind = k, v, kind
+        self._past = torch.zeros(self.batch, dtype=torch.int64, device=k.device)
         self.seen = 0
+        self._spec = E.TokenCacheSpec(F32 if dtype == "f32" else BF16, self.batch, self.kv_heads, self.head_dim,
+                                      self.sinks, self.capacity, k.data_ptr(), v.data_ptr(), self._past.data_ptr())
+
+    # the library's description of the cache holds their addresses: they are filled, not replaced
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
+    past = property(lambda self: self._past)
 
     def seek(self, past: Sequence[int]) -> None:
         """Streams that have seen past[b] tokens (0 for all: a new start)."""
-        import torch
         past = [int(p) for p in past]
         if len(past) != self.batch or min(past) < 0:
             raise ValueError("one number of tokens per stream")
         self.past.copy_(torch.tensor(past, dtype=torch.int64))
         self.seen = max(past)
 
-    def _spec(self):
-        return E.TokenCacheSpec(F32 if self.dtype == "f32" else BF16, self.batch, self.kv_heads, self.head_dim,
-                                self.sinks, self.capacity, self.k.data_ptr(), self.v.data_ptr(), self.past.data_ptr())
-
     def _rows(self, tokens: int, start, max_new: Optional[int]):
-        import torch
         if start is None:
             if tokens % self.batch or (max_new is not None and max_new * self.batch != tokens):
                 raise ValueError("without start every stream brings the same number of tokens")
@@ -220,7 +230,6 @@ class TokenCache:
         keys and values, put into the cache at past[b] onwards.  Query and key
         heads are normalised (root mean square, q_weight and k_weight
         [head_dim]; None: not) and turned by pos (int32 [tokens, axes])."""
-        import torch
         index, dim = self.index, self.head_dim
         _require(qkv, "qkv", self.kind, index)
         if q_heads < 1 or qkv.dim() != 2:
@@ -243,7 +252,7 @@ class TokenCache:
         spec = E.HeadSpec(q_heads, axes, rotary.section, rotary.interleaved, eps, ld)
         _launch(lib().sscater_tokens_append, "sscater_tokens_append", index, stream,
                 (qkv, pos, rotary.inv_freq, q_weight, k_weight, start, out, self.k, self.v, self.past), spec,
-                self._spec(), rows, qkv.data_ptr(), qw, kw, freq, at, out.data_ptr())
+                self._spec, rows, qkv.data_ptr(), qw, kw, freq, at, out.data_ptr())
         return out
 
     def attend(self, q, window: int, start=None, max_new: Optional[int] = None, causal: bool = True,
@@ -268,11 +277,10 @@ class TokenCache:
             raise ValueError("out must be on a 16-byte boundary")
         spec = E.AttendSpec(q.shape[1], min(int(window), 2 ** 31 - 1), 1 if causal else 0,
                             self.head_dim ** -0.5 if scale is None else scale)
-        cache, need, work = self._spec(), ctypes.c_size_t(), None
+        cache, need, work = self._spec, ctypes.c_size_t(), None
         _check(lib().sscater_tokens_workspace(spec, cache, rows, need), "sscater_tokens_workspace")
         if need.value:
-            import torch
-            work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+            work = q.new_empty(need.value, dtype=torch.uint8)
         _launch(lib().sscater_tokens_attend, "sscater_tokens_attend", index, stream,
                 (q, start, out, work, self.k, self.v, self.past), spec, cache, rows, q.data_ptr(), out.data_ptr(),
                 None if work is None else work.data_ptr(), need.value)
@@ -282,5 +290,5 @@ class TokenCache:
         """The call's tokens become past ones."""
         rows = self._rows(int(tokens), start, max_new)
         _launch(lib().sscater_tokens_advance, "sscater_tokens_advance", self.index, stream, (start, self.past),
-                self._spec(), rows)
+                self._spec, rows)
         self.seen += rows.max_new
