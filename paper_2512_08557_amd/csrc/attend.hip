@@ -30,7 +30,6 @@
 
 namespace ssc {
 
-typedef float f16v __attribute__((ext_vector_type(16)));
 typedef short s4v __attribute__((ext_vector_type(4)));
 
 struct AttendArgs {
@@ -51,18 +50,27 @@ template <bool F32, int D, int WM>
 struct AttendShape {
     static constexpr int S = F32 ? 4 : 2;
     static constexpr int RB = D * S;               // bytes of a cache row
-    static constexpr int CPR = RB / 16;            // its 16-byte pieces
-    static constexpr int BN = F32 || WM == 1 ? 32 : 64;   // keys of a tile
+    // fp32 with many rows: keys, values, queries and probabilities as three bf16
+    // planes and six of the nine products (as in the linear layers).  K and V are
+    // split once per workgroup on their way into LDS, through registers.
+    static constexpr bool PL = F32 && WM == 4;
+    static constexpr int NP = PL ? 3 : 1;          // planes
+    static constexpr int LRB = PL ? D * 2 : RB;    // bytes of a row in LDS
+    static constexpr int CPR = LRB / 16;           // its 16-byte pieces
+    static constexpr bool B16 = !F32 || PL;        // bf16 operands
+    static constexpr int BN = PL ? (D == 32 ? 64 : 32) : F32 || WM == 1 ? 32 : 64;   // keys of a tile
     static constexpr int NT = BN / 32;
-    static constexpr int TB = BN * RB;             // bytes of a tile
+    static constexpr int PB = BN * LRB;            // bytes of a plane
+    static constexpr int TB = NP * PB;             // bytes of a tile
+    static constexpr int NG = BN * RB / 16 / 256;  // pieces of a tile that a thread splits (PL)
     static constexpr int WK = 4 / WM;              // groups over keys
     static constexpr int BM = 32 * WM;
-    static constexpr int QN = RB / 32;             // 16-byte pieces of a lane's half of a query row
+    static constexpr int QN = LRB / 32;            // 16-byte pieces of a lane's half of a query row, of each plane
     static constexpr int ON = D / 2;               // output values of a lane
     static constexpr int GROUP = 4 * TB;           // two tiles of keys and two of values
     static constexpr int LDS = WK * GROUP > 4 * ON * 256 || WK == 1 ? WK * GROUP : 4 * ON * 256;
-    static constexpr int WGS = LDS > 80 * 1024 || (F32 && D == 128) ? 1 : 2;   // workgroups of a compute unit
-    static constexpr int RPC = 1024 / RB;          // rows of a copy
+    static constexpr int WGS = LDS > 80 * 1024 || (F32 && D >= 64) ? 1 : 2;   // workgroups of a compute unit
+    static constexpr int RPC = 1024 / LRB;         // rows of a copy
     static constexpr int NC = TB / 1024 / WM;      // copies of a wavefront for a tile of keys, and of values
     // Piece c of row r sits at piece c ^ swap: sixteen lanes that read one piece
     // of neighbouring rows (K), and the four rows of a transposed read by 32 lanes
@@ -72,7 +80,7 @@ struct AttendShape {
         return CPR == 4 ? (r >> 2) & 3 : CPR == 8 ? (r >> 1) & 7 : r & 15;
     }
     static __device__ __forceinline__ int swap_v(int r) {
-        if (F32) return CPR == 8 ? 0 : (r & 4) * 2;
+        if (!B16) return CPR == 8 ? 0 : (r & 4) * 2;
         return CPR == 4 ? 0 : CPR == 8 ? (r & 2) * 2 : (r & 3) * 4;
     }
 };
@@ -93,6 +101,31 @@ __device__ __forceinline__ int slot_of(const AttendArgs& a, const Reach& r, int 
     return a.sinks + min(x, ring - 1);
 }
 
+// Whether one of four values is infinite or NaN.
+__device__ __forceinline__ bool special(const uint4 v) {
+    const uint32_t m = 0x7F800000u;
+    return (v.x & m) == m || (v.y & m) == m || (v.z & m) == m || (v.w & m) == m;
+}
+
+// Eight values, signs flipped by `flip`, as operands of the three planes.
+__device__ __forceinline__ void split8(const uint4 lo, const uint4 hi, uint32_t flip, uint4 (&f)[3], bool& bad) {
+    bad |= special(lo) || special(hi);
+    cut_pair(lo.x ^ flip, lo.y ^ flip, f[0].x, f[1].x, f[2].x);
+    cut_pair(lo.z ^ flip, lo.w ^ flip, f[0].y, f[1].y, f[2].y);
+    cut_pair(hi.x ^ flip, hi.y ^ flip, f[0].z, f[1].z, f[2].z);
+    cut_pair(hi.z ^ flip, hi.w ^ flip, f[0].w, f[1].w, f[2].w);
+}
+
+// The six products of two operands in planes, the small ones first.
+__device__ __forceinline__ f16v mfma_planes(const uint4 (&x)[3], const uint4 (&y)[3], f16v c) {
+    c = mfma32(x[2], y[0], c);
+    c = mfma32(x[0], y[2], c);
+    c = mfma32(x[1], y[1], c);
+    c = mfma32(x[1], y[0], c);
+    c = mfma32(x[0], y[1], c);
+    return mfma32(x[0], y[0], c);
+}
+
 template <bool F32, int D, int WM>
 __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_kernel(AttendArgs a) {
     using C = AttendShape<F32, D, WM>;
@@ -101,12 +134,25 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wk = wave / WM;
     const int h = lane >> 5, col = lane & 31;
-    int id = blockIdx.x;
-    const int split = id % a.splits;
-    id /= a.splits;
-    const int tile = id % a.qtiles;
-    id /= a.qtiles;
-    const int kvh = id % a.kv_heads, b = id / a.kv_heads;
+    // Key heads go fastest, so that an XCD (workgroup id mod 8) keeps to one or a few of them and finds their keys in
+    // its L2; the last tokens' tiles, which reach furthest, come first, and short ones fill up the end.  Of few rows
+    // nothing is read twice: there splits go fastest, and every XCD has a part of each sequence, long or short (16 ragged
+    // streams over 65536 keys 190 us, with key heads fastest 215).
+    int id = blockIdx.x, kvh, b, split, tile;
+    if constexpr (WM == 1) {
+        split = id % a.splits;
+        id /= a.splits;
+        tile = 0;
+        kvh = id % a.kv_heads;
+        b = id / a.kv_heads;
+    } else {
+        kvh = id % a.kv_heads;
+        id /= a.kv_heads;
+        b = id % a.rows.batch;
+        id /= a.rows.batch;
+        split = id % a.splits;
+        tile = a.qtiles - 1 - id / a.splits;
+    }
     int first, n;
     rows_of(a.rows, b, first, n);
     const int nr = n * a.group;                    // rows of this key head
@@ -130,16 +176,26 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                               reach.n_sinks + (a.causal ? past + tok : past + n - 1) - reach.lo);
     const int from = (int)max((int64_t)0, reach.n_sinks + (a.causal ? past + tok : past) - a.window + 1 - reach.lo);
 
-    uint4 qf[C::QN];
-    {
+    bool again = false;                            // infinities or NaN: see the end of the tiles
+    uint4 qf[C::QN][C::NP];
+    if constexpr (C::PL) {
+        const char* p = (const char*)a.q + qrow * C::RB + h * 32;
+        bool bad = false;
+#pragma unroll
+        for (int s = 0; s < C::QN; ++s) {
+            const uint4 lo = *(const uint4*)(p + s * 64), hi = *(const uint4*)(p + s * 64 + 16);
+            split8(lo, hi, a.flip, qf[s], bad);
+        }
+        again = __ballot(bad) != 0;
+    } else {
         const char* p = (const char*)a.q + qrow * C::RB + h * 16;
 #pragma unroll
         for (int s = 0; s < C::QN; ++s) {
-            qf[s] = *(const uint4*)(p + s * 32);
-            qf[s].x ^= a.flip;
-            qf[s].y ^= a.flip;
-            qf[s].z ^= a.flip;
-            qf[s].w ^= a.flip;
+            qf[s][0] = *(const uint4*)(p + s * 32);
+            qf[s][0].x ^= a.flip;
+            qf[s][0].y ^= a.flip;
+            qf[s][0].z ^= a.flip;
+            qf[s][0].w ^= a.flip;
         }
     }
     f16v o[D / 32];
@@ -161,15 +217,22 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     // Copies of a tile: a lane's place within it is always the same, so for keys
     // that lie one behind the other only the uniform base moves.
     const int row0 = wm * C::RPC + lane / C::CPR, pc = lane % C::CPR;
-    // all copies of tile t's keys or values
-    auto copy = [&](int t, const char* from, auto value, lds_char* to) __attribute__((always_inline)) {
-        constexpr bool V = decltype(value)::value;
+    // Whether tile t's keys lie one behind the other, from cache row `row` on: not
+    // where the ring's end, the sinks' end or the last key cuts it.
+    auto whole = [&](int t, int& row) __attribute__((always_inline)) {
         const int u = t * C::BN, ring = a.capacity - a.sinks;
         int x = reach.base + (u - a.sinks);
         if (x >= ring) x -= ring;
         const bool sink = u + C::BN <= a.sinks;
-        if (u + C::BN <= reach.total && (sink || (u >= a.sinks && x + C::BN <= ring))) {
-            from += (int64_t)(sink ? u : a.sinks + x) * C::RB;
+        row = sink ? u : a.sinks + x;
+        return u + C::BN <= reach.total && (sink || (u >= a.sinks && x + C::BN <= ring));
+    };
+    // all copies of tile t's keys or values
+    auto copy = [&](int t, const char* from, auto value, lds_char* to) __attribute__((always_inline)) {
+        constexpr bool V = decltype(value)::value;
+        int row;
+        if (whole(t, row)) {
+            from += (int64_t)row * C::RB;
 #pragma unroll
             for (int j = 0; j < C::NC; ++j) {
                 const int r = j * (WM * C::RPC) + row0;
@@ -177,7 +240,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                        to + (j * WM + wm) * 1024);
             }
         } else {
-            // the ring's end, the sinks' end or the last key cuts it
+            const int u = t * C::BN;
 #pragma unroll 1
             for (int j = 0; j < C::NC; ++j) {
                 const int r = j * (WM * C::RPC) + row0;
@@ -185,6 +248,35 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                 copy16(from + at + (pc ^ (V ? C::swap_v(r) : C::swap_k(r))) * 16, to + (j * WM + wm) * 1024);
             }
         }
+    };
+    // PL: a thread's pieces of tile t, and their planes into LDS
+    auto fetch = [&](int t, const char* from, uint4 (&g)[C::NG > 0 ? C::NG : 1]) __attribute__((always_inline)) {
+        int row;
+        if (whole(t, row)) {
+            from += (int64_t)row * C::RB;
+#pragma unroll
+            for (int i = 0; i < C::NG; ++i) g[i] = *(const uint4*)(from + (uint32_t)(threadIdx.x + 256 * i) * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < C::NG; ++i) {
+                const int at = threadIdx.x + 256 * i, r = at / (C::RB / 16), p = at % (C::RB / 16);
+                g[i] = *(const uint4*)(from + p * 16 +
+                                       (int64_t)slot_of(a, reach, min(t * C::BN + r, reach.total - 1)) * C::RB);
+            }
+        }
+    };
+    bool bad = false;
+    auto spread = [&](const uint4 g, int i, auto value, lds_char* to) __attribute__((always_inline)) {
+        constexpr bool V = decltype(value)::value;
+        typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+        const int at = threadIdx.x + 256 * i, r = at / (C::RB / 16), p = at % (C::RB / 16);
+        bad |= special(g);
+        uint32_t w[3][2];
+        cut_pair(g.x, g.y, w[0][0], w[1][0], w[2][0]);
+        cut_pair(g.z, g.w, w[0][1], w[1][1], w[2][1]);
+        lds_char* dst = to + r * C::LRB + ((p >> 1) ^ (V ? C::swap_v(r) : C::swap_k(r))) * 16 + (p & 1) * 8;
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *(__attribute__((address_space(3))) u2v*)(dst + q * C::PB) = u2v{w[q][0], w[q][1]};
     };
     // the group's tiles are tb + wk, tb + wk + WK, ...; groups that share a workgroup go round as often as the first
     const int mine = te - tb > wk ? (te - tb - wk + C::WK - 1) / C::WK : 0;
@@ -200,30 +292,36 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     lds_char* const vbuf = own + 2 * C::TB;
 
     constexpr int STEPS = C::NT * C::QN;               // of the product with the keys
-    auto key_step = [&](f16v (&s)[C::NT], int i, const uint4 kf) __attribute__((always_inline)) {
+    struct Operand {
+        uint4 p[C::NP];
+    };
+    auto key_step = [&](f16v (&s)[C::NT], int i, const Operand& k) __attribute__((always_inline)) {
         const int t = i / C::QN, c = i % C::QN;
-        if constexpr (F32) {
-            const uint32_t kv[4] = {kf.x, kf.y, kf.z, kf.w}, qv[4] = {qf[c].x, qf[c].y, qf[c].z, qf[c].w};
+        if constexpr (C::PL) {
+            s[t] = mfma_planes(k.p, qf[c], s[t]);
+        } else if constexpr (F32) {
+            const uint4 kf = k.p[0], q = qf[c][0];
+            const uint32_t kv[4] = {kf.x, kf.y, kf.z, kf.w}, qv[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 s[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kv[e]), __uint_as_float(qv[e]), s[t], 0, 0, 0);
         } else {
-            bf8v A, B;
-            __builtin_memcpy(&A, &kf, 16);
-            __builtin_memcpy(&B, &qf[c], 16);
-            s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, B, s[t], 0, 0, 0);
+            s[t] = mfma32(k.p[0], qf[c][0], s[t]);
         }
     };
     auto key_load = [&](const lds_char* kl, int i) __attribute__((always_inline)) {
         const int r = 32 * (i / C::QN) + col;
-        return lds16(kl + r * C::RB + ((2 * (i % C::QN) + h) ^ C::swap_k(r)) * 16);
+        Operand k;
+#pragma unroll
+        for (int p = 0; p < C::NP; ++p)
+            k.p[p] = lds16(kl + p * C::PB + r * C::LRB + ((2 * (i % C::QN) + h) ^ C::swap_k(r)) * 16);
+        return k;
     };
     auto clear = [&](f16v (&s)[C::NT]) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < C::NT; ++t) s[t] = f16v{};
     };
 
-    bool again = false;
     // Round j: the softmax of tile j's scores s beside the products that give tile
     // j + 1's, in n (a wavefront's vector instructions run while its matrix
     // instructions do, if they are next to each other), then the product with the
@@ -231,8 +329,15 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     auto round = [&](int j, auto parity, f16v (&s)[C::NT], f16v (&n)[C::NT]) __attribute__((always_inline)) {
         constexpr int P = decltype(parity)::value;
         meet();
-        if (j + 2 < mine) copy(tile_of(j + 2), kg, std::false_type{}, kbuf + P * C::TB);
-        if (j + 1 < mine) copy(tile_of(j + 1), vg, std::true_type{}, vbuf + (1 - P) * C::TB);
+        uint4 gk[C::NG > 0 ? C::NG : 1], gv[C::NG > 0 ? C::NG : 1];
+        if (j + 2 < mine) {
+            if constexpr (C::PL) fetch(tile_of(j + 2), kg, gk);
+            else copy(tile_of(j + 2), kg, std::false_type{}, kbuf + P * C::TB);
+        }
+        if (j + 1 < mine) {
+            if constexpr (C::PL) fetch(tile_of(j + 1), vg, gv);
+            else copy(tile_of(j + 1), vg, std::true_type{}, vbuf + (1 - P) * C::TB);
+        }
         const lds_char* kl = kbuf + (1 - P) * C::TB;
         const lds_char* vl = vbuf + P * C::TB;
         const int u0 = tile_of(j) * C::BN;
@@ -247,8 +352,11 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                     const int u = u0 + 32 * t + 8 * (e >> 2) + 4 * h + (e & 3);
                     s[t][e] = j < mine && u <= last && (u >= from || u < a.sinks) ? s[t][e] : -INFINITY;
                 }
+        }
+        if (!C::PL && masked) {
             // A masked key's probability is zero, but its values may be infinite
             // or NaN, and the matrix product would carry those to every row.
+            // (Planes find them as they are split, in every tile.)
             uint32_t big = 0;
 #pragma unroll 2
             for (int i = lane; i < C::TB / 16; i += 64) {
@@ -262,8 +370,9 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         }
         // (past the last tile these are products of what the buffer holds; nobody reads them)
         constexpr int FIRST = STEPS / 4;
-        constexpr int KA = STEPS < 4 ? 2 : 4;          // operands under way: LDS answers after about four products
-        uint4 kf[KA];
+        // operands under way: LDS answers after about four products
+        constexpr int KA = C::PL || STEPS < 4 ? 2 : 4;
+        Operand kf[KA];
 #pragma unroll
         for (int i = 0; i < KA - 1; ++i) kf[i] = key_load(kl, i);
         auto key_next = [&](int i) __attribute__((always_inline)) {
@@ -295,31 +404,34 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                 for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
         }
         const float ms = m == -INFINITY ? 0.f : m;
-        uint4 pf[C::NT * 2];                           // bf16: eight probabilities each
-        // the values of 16 keys (bf16) or of two (fp32), all of a head
-        constexpr int VS = F32 ? 16 : C::BN / 16, VA = F32 ? 4 : 2;
-        uint4 vf[VA][D / 32];
+        uint4 pf[C::NT * 2][C::NP];                    // bf16 operands: eight probabilities each
+        // the values of 16 keys (bf16 operands) or of two (fp32), all of a head
+        constexpr int VS = C::B16 ? C::BN / 16 : 16, VA = C::B16 ? 2 : 4;
+        Operand vf[VA][D / 32];
         auto value_load = [&](int ks) __attribute__((always_inline)) {
-            if constexpr (F32) {
+            if constexpr (!C::B16) {
                 const int key = 8 * (ks >> 2) + 4 * h + (ks & 3);
 #pragma unroll
                 for (int t = 0; t < D / 32; ++t) {
                     const int at = key * C::RB + (((8 * t + col / 4) ^ C::swap_v(key)) * 4 + col % 4) * 4;
-                    vf[ks % VA][t].x = *(const __attribute__((address_space(3))) uint32_t*)(vl + at);
+                    vf[ks % VA][t].p[0].x = *(const __attribute__((address_space(3))) uint32_t*)(vl + at);
                 }
             } else {
                 const int i = lane & 15, key = 16 * ks + 4 * h + (i >> 2);
                 // rows key and key + 8 have the same swap
-                const lds_char* at = vl + key * C::RB + 8 * (i & 1);
+                const lds_char* at = vl + key * C::LRB + 8 * (i & 1);
 #pragma unroll
-                for (int t = 0; t < D / 32; ++t) {
-                    const int c = (4 * t + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1)) ^ C::swap_v(key);
-                    typedef __attribute__((address_space(3))) s4v lds_s4v;
-                    const s4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + c * 16));
-                    const s4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + 8 * C::RB + c * 16));
-                    __builtin_memcpy(&vf[ks % VA][t], &v0, 8);
-                    __builtin_memcpy((char*)&vf[ks % VA][t] + 8, &v1, 8);
-                }
+                for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                    for (int p = 0; p < C::NP; ++p) {
+                        const int c = (4 * t + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1)) ^ C::swap_v(key);
+                        typedef __attribute__((address_space(3))) s4v lds_s4v;
+                        const s4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + p * C::PB + c * 16));
+                        const s4v v1 =
+                            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + p * C::PB + 8 * C::LRB + c * 16));
+                        __builtin_memcpy(&vf[ks % VA][t].p[p], &v0, 8);
+                        __builtin_memcpy((char*)&vf[ks % VA][t].p[p] + 8, &v1, 8);
+                    }
             }
         };
         constexpr int ALL = 16 * C::NT, LEFT = STEPS - FIRST;
@@ -332,13 +444,20 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                 const float x = __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], a.scale, -ms));
                 s[e >> 4][e & 15] = x;
                 l += x;
-                if (!F32 && (e & 1)) {
-                    const uint32_t w = bf16_pair(s[e >> 4][(e & 15) - 1], x);
-                    uint4& f = pf[e >> 3];
-                    if ((e & 7) == 1) f.x = w;
-                    else if ((e & 7) == 3) f.y = w;
-                    else if ((e & 7) == 5) f.z = w;
-                    else f.w = w;
+                if (C::B16 && (e & 1)) {
+                    uint32_t w[3];
+                    if constexpr (C::PL)
+                        cut_pair(__float_as_uint(s[e >> 4][(e & 15) - 1]), __float_as_uint(x), w[0], w[1], w[2]);
+                    else
+                        w[0] = bf16_pair(s[e >> 4][(e & 15) - 1], x);
+#pragma unroll
+                    for (int p = 0; p < C::NP; ++p) {
+                        uint4& f = pf[e >> 3][p];
+                        if ((e & 7) == 1) f.x = w[p];
+                        else if ((e & 7) == 3) f.y = w[p];
+                        else if ((e & 7) == 5) f.z = w[p];
+                        else f.w = w[p];
+                    }
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -350,14 +469,18 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
             if (ks + VA - 1 < VS) value_load(ks + VA - 1);
 #pragma unroll
             for (int t = 0; t < D / 32; ++t) {
-                const uint4 v = vf[ks % VA][t];
-                if constexpr (F32) {
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v.x), s[0][ks], o[t], 0, 0, 0);
-                } else {
-                    bf8v A, B;
-                    __builtin_memcpy(&A, &v, 16);
-                    __builtin_memcpy(&B, &pf[ks], 16);
-                    o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, B, o[t], 0, 0, 0);
+                const Operand& v = vf[ks % VA][t];
+                if constexpr (C::PL) o[t] = mfma_planes(v.p, pf[ks], o[t]);
+                else if constexpr (F32)
+                    o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v.p[0].x), s[0][ks], o[t], 0, 0, 0);
+                else o[t] = mfma32(v.p[0], pf[ks][0], o[t]);
+            }
+            if constexpr (C::PL) {
+                // the next tiles' planes beside the products
+#pragma unroll
+                for (int i = ks * C::NG / VS; i < (ks + 1) * C::NG / VS; ++i) {
+                    if (j + 2 < mine) spread(gk[i], i, std::false_type{}, kbuf + P * C::TB);
+                    if (j + 1 < mine) spread(gv[i], i, std::true_type{}, vbuf + (1 - P) * C::TB);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -366,17 +489,35 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
 
     f16v sa[C::NT], sb[C::NT];
     clear(sa);
-    if (mine > 0) copy(tile_of(0), kg, std::false_type{}, kbuf);
+    auto first_copy = [&](int t, const char* from, auto value, lds_char* to) __attribute__((always_inline)) {
+        if constexpr (C::PL) {
+            uint4 g[C::NG];
+            fetch(t, from, g);
+#pragma unroll
+            for (int i = 0; i < C::NG; ++i) spread(g[i], i, value, to);
+        } else {
+            copy(t, from, value, to);
+        }
+    };
+    if (mine > 0) first_copy(tile_of(0), kg, std::false_type{}, kbuf);
     meet();
     if (mine > 0) {
-        copy(tile_of(0), vg, std::true_type{}, vbuf);
-        if (mine > 1) copy(tile_of(1), kg, std::false_type{}, kbuf + C::TB);
+        first_copy(tile_of(0), vg, std::true_type{}, vbuf);
+        if (mine > 1) first_copy(tile_of(1), kg, std::false_type{}, kbuf + C::TB);
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) key_step(sa, i, key_load(kbuf, i));
     }
     for (int j = 0; j < rounds; j += 2) {
         round(j, std::integral_constant<int, 0>{}, sa, sb);
         if (j + 1 < rounds) round(j + 1, std::integral_constant<int, 1>{}, sb, sa);
+    }
+    if constexpr (C::PL) {
+        // a wavefront's share of the keys and values is every wavefront's concern
+        const float any = __ballot(bad) != 0 ? 1.f : 0.f;
+        if (lane == 0) ml[wave][0][0] = any;
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < 4; ++g) again |= ml[g][0][0] != 0.f;
     }
     if (again) {
         // Keys one by one, each only for the rows that see it: the wavefront's
@@ -392,7 +533,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
             const int64_t at = (int64_t)slot_of(a, reach, u) * C::RB;
             float x = 0.f;
 #pragma unroll 1
-            for (int c = 0; c < C::CPR; ++c) {
+            for (int c = 0; c < C::RB / 16; ++c) {
                 uint4 qv = *(const uint4*)(qr + c * 16), kv = *(const uint4*)(kg + at + c * 16);
                 const uint32_t qw[4] = {qv.x ^ a.flip, qv.y ^ a.flip, qv.z ^ a.flip, qv.w ^ a.flip};
                 const uint32_t kw[4] = {kv.x, kv.y, kv.z, kv.w};
@@ -526,6 +667,19 @@ __global__ __launch_bounds__(256) void join_kernel(const float* part, void* out,
 
 namespace {
 
+// Workgroups of attend_kernel that a compute unit takes.
+template <bool F32, int D>
+int attend_places(int wm) {
+    if constexpr (!(F32 && D == 128))
+        if (wm == 1) return AttendShape<F32, D, 1>::WGS;
+    return wm == 2 ? AttendShape<F32, D, 2>::WGS : AttendShape<F32, D, 4>::WGS;
+}
+
+int attend_places(bool f32, int dim, int wm) {
+    if (f32) return dim == 32 ? attend_places<true, 32>(wm) : dim == 64 ? attend_places<true, 64>(wm) : attend_places<true, 128>(wm);
+    return dim == 32 ? attend_places<false, 32>(wm) : dim == 64 ? attend_places<false, 64>(wm) : attend_places<false, 128>(wm);
+}
+
 // How a call is cut up, from what the host knows.
 struct AttendCut {
     int wm, qtiles, splits;
@@ -546,10 +700,26 @@ bool attend_cut(const sscater_attend_spec* s, const sscater_token_cache* c, cons
     cut->qtiles = (int)((rows + 32 * cut->wm - 1) / (32 * cut->wm));
     const int64_t base = (int64_t)cut->qtiles * c->kv_heads * c->batch;
     const int64_t keys = reach + c->sinks;
-    const int bn = (c->dtype == SSCATER_F32 || cut->wm == 1 ? 32 : 64) * (4 / cut->wm);
+    const int bn = (cut->wm == 1 || (c->dtype == SSCATER_F32 && !(cut->wm == 4 && c->head_dim == 32)) ? 32 : 64) * (4 / cut->wm);
+    // Splits of the keys, of two tiles for each group at least.  Few rows are bound by the cache's bytes: two workgroups
+    // for every compute unit.  Otherwise the number that makes the share of a full card times its passes least; each
+    // split costs its sums' way through memory, about a hundredth (216 tiles of fp32: in three, 648 workgroups on 512
+    // places, 942 us; in seven, three nearly full passes, 806).
+    const int64_t most = std::max((int64_t)1, std::min((keys + 2 * bn - 1) / (2 * bn), (int64_t)MAX_SPLITS));
     cut->splits = 1;
-    if (base > 0 && base < 256)
-        cut->splits = (int)std::max((int64_t)1, std::min({(512 + base - 1) / base, (keys + 2 * bn - 1) / (2 * bn), (int64_t)MAX_SPLITS}));
+    if (base > 0 && cut->wm == 1) {
+        if (base < 256) cut->splits = (int)std::min((512 + base - 1) / base, most);
+    } else if (base > 0) {
+        const int64_t places = 256 * attend_places(c->dtype == SSCATER_F32, c->head_dim, cut->wm);
+        double best = 0.;
+        for (int64_t n = 1; base < 2 * places && n <= most; ++n) {
+            const double cost = (double)((base * n + places - 1) / places) / n + (n > 1 ? 0.01 * n * base / places : 0.);
+            if (n == 1 || cost < best) {
+                best = cost;
+                cut->splits = (int)n;
+            }
+        }
+    }
     cut->grid = base * cut->splits;
     return cut->grid <= 0x7FFFFFFF;
 }

@@ -18,8 +18,6 @@
 
 namespace ssc {
 
-typedef float f16v __attribute__((ext_vector_type(16)));
-
 struct LinearArgs {
     const void* x;
     const void* w;
@@ -93,23 +91,6 @@ __device__ __forceinline__ float load_value(const void* p, int64_t i) {
     return __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16);
 }
 
-// The three planes of two values by cutting off: x in the low halves.
-__device__ __forceinline__ void cut_pair(uint32_t x, uint32_t y, uint32_t& h, uint32_t& m, uint32_t& l) {
-    const float rx = __uint_as_float(x) - __uint_as_float(x & 0xFFFF0000u);
-    const float ry = __uint_as_float(y) - __uint_as_float(y & 0xFFFF0000u);
-    h = __builtin_amdgcn_perm(y, x, 0x07060302u);
-    const uint32_t ux = __float_as_uint(rx), uy = __float_as_uint(ry);
-    m = __builtin_amdgcn_perm(uy, ux, 0x07060302u);
-    const float sx = rx - __uint_as_float(ux & 0xFFFF0000u), sy = ry - __uint_as_float(uy & 0xFFFF0000u);
-    l = __builtin_amdgcn_perm(__float_as_uint(sy), __float_as_uint(sx), 0x07060302u);
-}
-
-__device__ __forceinline__ f16v mfma32(uint4 a, uint4 b, f16v c) {
-    bf8v A, B;
-    __builtin_memcpy(&A, &a, 16);
-    __builtin_memcpy(&B, &b, 16);
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(A, B, c, 0, 0, 0);
-}
 
 // Channels k.. of a row that starts at value `at` and may be aligned to its values
 // only: 16 bytes, zeros from channel K on.
