@@ -212,7 +212,10 @@ class TokenCache:
         past = [int(p) for p in past]
         if len(past) != self.batch or min(past) < 0:
             raise ValueError("one number of tokens per stream")
-        self.past.copy_(torch.tensor(past, dtype=torch.int64))
+        if min(past) == max(past):
+            self._past.fill_(past[0])
+        else:
+            self._past.copy_(torch.tensor(past, dtype=torch.int64))
         self.seen = max(past)
 
     def _rows(self, tokens: int, start, max_new: Optional[int]):
