@@ -1,13 +1,22 @@
 // Linear layers over rows of cells: y = act(x W^T + b) + r.
 //
-// A workgroup of four wavefronts owns a tile of 128 rows and 128 output
-// channels, a wavefront 64 x 64 of it as 2 x 2 blocks of 32 x 32.  K runs in
-// steps through two LDS stages.  W is the first matrix operand and x the
-// second, so a lane holds four consecutive output channels of one row.
+// W is the first matrix operand and x the second, so a lane holds four
+// consecutive output channels of one row; sums are fp32, rounded once.  Four
+// kernels, by the number of rows and channels:
+//   few rows      linear_rows_kernel: K shared by the wavefronts, no LDS on the way
+//                 in (4 x 256 -> 1024 bf16: 3.0 us, a launch and two round trips);
+//   some rows     linear_kernel: tiles of 64 x 64, 128 x 128 or 128 x 64 through LDS
+//                 (12000 x 1024 -> 256 fp32 with residual 48 us, 132 TFLOP/s; a head of
+//                 42 channels over 53568 x 384 bf16 11.6 us, 3.9 TB/s);
+//   many, in bf16 linear_big_kernel: persistent tiles of 256 x 128
+//                 (214272 x 384 -> 1536 344 us, with gelu 410; 8192^3 1115 us,
+//                 986 TFLOP/s, two thirds of a library product's rate).
 //
 // fp32: a step's values are split in registers into three bf16 planes of 8
 // bits each by cutting off (h + m + l is the value exactly), and six of the
-// nine products are formed; the others are at most 2^-23 of the whole.
+// nine products are formed; the others are at most 2^-23 of the whole.  Six bf16
+// instructions take 0.4 of the fp32 kind's time.  An infinity leaves NaN in its
+// lower planes: a NaN sum is formed again from the values.
 #include <hip/hip_runtime.h>
 
 #include "../../include/sscater.h"
@@ -41,9 +50,9 @@ __device__ __attribute__((aligned(16))) uint32_t linear_zero[4];
 // z (1 + erf(z / sqrt 2)) / 2 = max(z, 0) - |z| Phi(-|z|), with log2 Phi(-t) as a
 // polynomial in t (fitted for 0 <= t <= 5.5 by weighted least squares, the
 // weights moved until Phi's error was level): |error of Phi| <= 4e-8, which is
-// also what stays from there on.  60 clocks of a wavefront, 16 of them the one
-// transcendental instruction; the layers that end in it are bound by this.  (By
-// erfc's rational approximation in 1 / (1 + p t) 80.)
+// also what stays from there on.  Eleven vector instructions and one exponential,
+// some 57 clocks of a wavefront (4.4 and 8.6 each, measured); erfc's rational
+// approximation in 1 / (1 + p t) takes 80.
 __device__ __forceinline__ float gelu(float z) {
     const float t = fminf(fabsf(z), 5.5f);
     float p = fmaf(8.470141e-06f, t, -5.3903543e-05f);
@@ -232,8 +241,10 @@ __device__ __forceinline__ void put_edge(const LinearArgs& a, const f16v& acc, c
 // together (straight from the sums' layout a store is 32 rows of 32 bytes, which
 // the memory path takes at a quarter of its rate), and the residual comes the
 // other way through the same place.  bf16: lanes r and r + 32 hold the two halves
-// of eight channels and swap halves of two groups first.
-template <bool F32, int ACT, int NI>
+// of eight channels and swap halves of two groups first.  PAST: the stores pass by
+// the caches, where the output is larger than they are (four maps' 384 -> 1536
+// layer 389 -> 344 us: x and W stay in L2).
+template <bool F32, int ACT, int NI, bool PAST>
 __device__ __forceinline__ void put_rows(const LinearArgs& a, const f16v (&acc)[NI], const lds_float* bias,
                                          lds_char* own, int64_t m, int n) {
     constexpr int S = F32 ? 4 : 2, RB = 32 * NI * S, L = RB / 16, RPI = 64 / L;   // lanes of a row, rows of a store
@@ -298,8 +309,12 @@ __device__ __forceinline__ void put_rows(const LinearArgs& a, const f16v (&acc)[
         for (int g = 0; g < S; ++g) *(lds_u4v*)(own + place<RB>(r, 2 * S * i + 2 * g + h)) = out[i][g];
     char* to = (char*)a.y + ((m + lane / L) * a.ldy + n) * S + lane % L * 16;
 #pragma unroll
-    for (int i = 0; i < 32 / RPI; ++i)
-        *(u4v*)(to + (int64_t)i * RPI * a.ldy * S) = *(const lds_u4v*)(own + place<RB>(i * RPI + lane / L, lane % L));
+    for (int i = 0; i < 32 / RPI; ++i) {
+        const u4v v = *(const lds_u4v*)(own + place<RB>(i * RPI + lane / L, lane % L));
+        u4v* y = (u4v*)(to + (int64_t)i * RPI * a.ldy * S);
+        if constexpr (PAST) __builtin_nontemporal_store(v, y);
+        else *y = v;
+    }
 }
 
 // 32 rows of a matrix of few channels that lie one behind the other (no more than
@@ -327,7 +342,7 @@ __device__ __forceinline__ void put_packed(const LinearArgs& a, const f16v (&acc
 }
 
 // A wavefront's TM x TN blocks; own: 4 KB of LDS that no other wavefront uses.
-template <bool F32, int ACT, bool FULL, int TM, int TN>
+template <bool F32, int ACT, bool FULL, int TM, int TN, bool PAST>
 __device__ __forceinline__ void put_blocks(const LinearArgs& a, const f16v (&acc)[TN][TM], const lds_float* bias,
                                            lds_char* own, int64_t m, int n) {
     const int r = threadIdx.x & 31, h = threadIdx.x >> 5 & 1;
@@ -340,7 +355,7 @@ __device__ __forceinline__ void put_blocks(const LinearArgs& a, const f16v (&acc
                 f16v z[NI];
 #pragma unroll
                 for (int c = 0; c < NI; ++c) z[c] = acc[i + c][j];
-                put_rows<F32, ACT, NI>(a, z, bias + 32 * i, own, m + 32 * j, n + 32 * i);
+                put_rows<F32, ACT, NI, PAST>(a, z, bias + 32 * i, own, m + 32 * j, n + 32 * i);
             } else {
 #pragma unroll
                 for (int c = 0; c < NI; ++c)
@@ -527,8 +542,8 @@ __global__ __launch_bounds__(256, 2) void linear_kernel(LinearArgs a) {
                 return;
             }
         }
-        put_blocks<F32, decltype(act)::value, decltype(full)::value, TM, TN>(a, acc, (const lds_float*)bias + wn, own,
-                                                                             m0 + wm, n0 + wn);
+        put_blocks<F32, decltype(act)::value, decltype(full)::value, TM, TN, false>(
+            a, acc, (const lds_float*)bias + wn, own, m0 + wm, n0 + wn);
     };
     put_tile(a, m0 + C::BM <= a.M && n0 + C::BN <= a.N, put);
 }
@@ -644,7 +659,7 @@ __global__ __launch_bounds__(512) void linear_big_kernel(LinearArgs a) {
         lds_barrier();
         lds_char* own = lds + (slot == 0 ? C::NST - 1 : slot - 1) * C::STAGE + wave * 4096;
         auto put = [&](auto act, auto full) __attribute__((always_inline)) {
-            put_blocks<false, decltype(act)::value, decltype(full)::value, 2, 2>(
+            put_blocks<false, decltype(act)::value, decltype(full)::value, 2, 2, true>(
                 a, acc, (const lds_float*)bias[side] + wn, own, m0 + wm, n0 + wn);
         };
         put_tile(a, m0 + C::BM <= a.M && n0 + C::BN <= a.N, put);
