@@ -41,9 +41,6 @@ struct LinearArgs {
     int rvec, yvec;       // residual and output rows may be accessed 16 bytes at a time
 };
 
-// Fewer tiles of 64 x 64 than these take linear_rows_kernel.
-constexpr int FEW_TILES = 160;
-
 // What a copy reads where its tile has nothing.
 __device__ __attribute__((aligned(16))) uint32_t linear_zero[4];
 
@@ -778,22 +775,33 @@ bool launch_big(LinearArgs& a, hipStream_t s) {
 
 template <bool F32, bool VEC>
 bool launch_linear(LinearArgs& a, hipStream_t s) {
-    const int64_t n16 = (a.N + 15) / 16, n32 = (a.N + 31) / 32, few = (a.M + 63) / 64 * ((a.N + 63) / 64);
-    if (a.M <= 64 || few < FEW_TILES) {
+    // Which kernel, by how many tiles there are for 256 compute units (us on either side of each bound):
+    // fewer than 128 tiles of 64 x 64 leave units idle for all of K, so K is shared (500 x 512 -> 512 fp32, 64 tiles: rows
+    // 9.8, tiles 17.0; 600 x 1024 -> 1024 bf16, 160 tiles: rows 13.6, tiles 10.4); the rows kernel's larger block from 512
+    // blocks on (64 x 1536 -> 1536, 384 of them: one 7.5, larger 8.3; 128 rows, 768: 10.2 and 8.4)
+    const int64_t n16 = (a.N + 15) / 16, n32 = (a.N + 31) / 32;
+    if (a.M <= 64 || (a.M + 63) / 64 * ((a.N + 63) / 64) < 128) {
         const int64_t small = (a.M + 15) / 16 * n16;
-        const bool one = small <= 1024;
+        const bool one = small <= 512;
         a.tn = (int)(one ? n16 : n32);
         const dim3 grid((unsigned)(one ? small : (a.M + 31) / 32 * n32));
         if (one) linear_rows_kernel<F32, VEC, 1><<<grid, dim3(256), 0, s>>>(a);
         else linear_rows_kernel<F32, VEC, 2><<<grid, dim3(256), 0, s>>>(a);
         return true;
     }
-    const int64_t big = ((a.M + 127) / 128) * ((a.N + 127) / 128);
-    if constexpr (!F32 && VEC)
-        if (a.N > 64 && big >= 1024) return launch_big(a, s);
+    // the persistent kernel where its passes over the card are nearly full (53568 x 384 -> 384, 630 of 768 places: 29.3,
+    // tiles of 128 31.9; 24000 x 256 -> 512, 376 of 512: 23.5 and 17.7), a little less so for a long K (8192 x 1536 ->
+    // 1536, 384 of 512: 52.2 and 60.2)
+    if constexpr (!F32 && VEC) {
+        const int64_t tiles = (a.M + BigShape::BM - 1) / BigShape::BM * ((a.N + BigShape::BN - 1) / BigShape::BN);
+        const int64_t places = (tiles + 255) / 256 * 256;
+        if (a.N > 64 && (tiles * 5 >= places * 4 || (tiles * 10 >= places * 7 && a.K >= 1024))) return launch_big(a, s);
+    }
     // a tile of all channels, unless rows of exactly 64 can be stored as they are
     if (a.N <= 64 && !(a.N == 64 && a.yvec) && a.M >= 256 * 64) return launch_tiles<F32, VEC, 4, 1, 1, 2>(a, s);
-    if (big >= 256 && a.N > 64) return launch_tiles<F32, VEC, 2, 2, 2, 2>(a, s);
+    // 128 x 128 from 400 of them on (12000 x 256 -> 512 bf16, 376: 13.4, 64 x 64 10.1; 30000 x 1536 -> 256, 470: 33.2 and
+    // 43.8; 12000 x 1024 -> 256 fp32, 188: 63.7 and 50.7)
+    if (a.N > 64 && (a.M + 127) / 128 * ((a.N + 127) / 128) >= 400) return launch_tiles<F32, VEC, 2, 2, 2, 2>(a, s);
     return launch_tiles<F32, VEC, 2, 2, 1, 1>(a, s);
 }
 

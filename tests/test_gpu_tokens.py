@@ -94,6 +94,19 @@ def test_linear_many_rows(rows, cin, cout, kind):
         close(ssc.linear(x, w, bias, activation=act, residual=res), *linear_ref(x, w, bias, act, res, kind), act)
 
 
+@pytest.mark.parametrize("rows,cin,cout", [(65000, 72, 500), (60000, 200, 384), (27500, 8, 130), (65024, 64, 512),
+                                           (27000, 136, 128)])
+def test_linear_over_full_passes(rows, cin, cout):
+    """Sizes whose tiles of 256 x 128 fill the card once or several times, ragged
+    and whole, one to four steps of K."""
+    note(f"[gpu-test] linear {rows} {cin} {cout}")
+    rng = np.random.default_rng(rows + cin + cout)
+    x, w = normal(rng, (rows, cin), torch.bfloat16), normal(rng, (cout, cin), torch.bfloat16, cin ** -0.5)
+    b, r = normal(rng, (cout,), torch.bfloat16), normal(rng, (rows, cout), torch.bfloat16)
+    for act, bias, res in (("gelu", b, None), ("none", None, r)):
+        close(ssc.linear(x, w, bias, activation=act, residual=res), *linear_ref(x, w, bias, act, res, "bf16"), act)
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("pad,offset", [(0, 1), (1, 0), (8, 0), (8, 8), (3, 5), (64, 0)])
 def test_linear_strides_and_alignment(kind, pad, offset):
