@@ -609,13 +609,17 @@ __global__ __launch_bounds__(512) void linear_big_kernel(LinearArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) issue(i & 3);
     wait_vm<0>();
+    // A tile's bias comes with the last step of the tile before: awaited at its start it would wait for that one's
+    // stores as well.
+    auto bias_of = [&](int t) __attribute__((always_inline)) {
+        const int n = t % a.tn * C::BN + threadIdx.x;
+        return a.bias && t < end && (int)threadIdx.x < C::BN && n < a.N ? load_value<false>(a.bias, n) : 0.f;
+    };
+    if ((int)threadIdx.x < C::BN) bias[0][threadIdx.x] = bias_of(first);
     int slot = 0, side = 0;
     for (int t = first; t < end; t += stride, side ^= 1) {
         const int64_t m0 = (int64_t)(t / a.tn) * C::BM;
         const int n0 = t % a.tn * C::BN;
-        if ((int)threadIdx.x < C::BN)
-            bias[side][threadIdx.x] =
-                a.bias && n0 + (int)threadIdx.x < a.N ? load_value<false>(a.bias, n0 + threadIdx.x) : 0.f;
         f16v acc[2][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -651,6 +655,8 @@ __global__ __launch_bounds__(512) void linear_big_kernel(LinearArgs a) {
             }
             slot = slot + 1 == C::NST ? 0 : slot + 1;
         }
+        const float next = bias_of(t + stride);
+        if ((int)threadIdx.x < C::BN) bias[side ^ 1][threadIdx.x] = next;
         wait_vm<0>();
         // the stage read last takes no copies before the next barrier but one
         lds_barrier();
