@@ -7,10 +7,10 @@
 //                 in (4 x 256 -> 1024 bf16: 3.0 us, a launch and two round trips);
 //   some rows     linear_kernel: tiles of 64 x 64, 128 x 128 or 128 x 64 through LDS
 //                 (12000 x 1024 -> 256 fp32 with residual 48 us, 132 TFLOP/s; a head of
-//                 42 channels over 53568 x 384 bf16 11.6 us, 3.9 TB/s);
+//                 42 channels over 53568 x 384 bf16 11.7 us, 3.9 TB/s);
 //   many, in bf16 linear_big_kernel: persistent tiles of 256 x 128
-//                 (214272 x 384 -> 1536 344 us, with gelu 410; 8192^3 1115 us,
-//                 986 TFLOP/s, two thirds of a library product's rate).
+//                 (214272 x 384 -> 1536 336 us, with gelu 414; 8192^3 1095 us,
+//                 1004 TFLOP/s, two thirds of a library product's rate).
 //
 // fp32: a step's values are split in registers into three bf16 planes of 8
 // bits each by cutting off (h + m + l is the value exactly), and six of the

@@ -7,7 +7,7 @@
 // (the same places of both halves of the head), whose sum of squares is
 // reduced between those lanes.  Every value is read and written once: 100000 fp32
 // tokens of 16 heads of 64 values 95 us, 5.1 TB/s, the rate of a copy; one token
-// 3.6 us, a launch, the positions' and the row's round trips.
+// 3.7 us, a launch, the positions' and the row's round trips.
 //
 // The angle in turns is position * inv_freq / (2 pi) in 64 bits less its whole
 // part: a stream's stride number passes 10^6 within hours, where 32 bits would
