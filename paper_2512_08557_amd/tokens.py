@@ -111,8 +111,8 @@ def linear(x, weight, bias=None, activation: Optional[str] = None, residual=None
     kind = _KINDS.get(dtype, -1)
     if kind < 0:
         raise ValueError(f"float32 or bfloat16 tensors, not {dtype}")
-    if weight.dim() != 2:
-        raise ValueError("weight must be [cout, cin]")
+    if weight.dim() != 2 or 0 in weight.shape:
+        raise ValueError("weight must be [cout, cin], of at least one channel each")
     cout, cin = weight.shape
     if not x.is_cuda:
         raise ValueError("x must be a cuda tensor")

@@ -175,3 +175,10 @@ def test_python_refusals():
             ssc.TokenCache(*args, **kw)
     with pytest.raises(ValueError, match="axes"):
         ssc.Rotary(None, (8, 8, 8, 8), device="cpu")
+
+
+@pytest.mark.parametrize("cout,cin", [(3, 0), (0, 8), (0, 0)])
+def test_python_linear_refuses_layers_without_channels(cout, cin):
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError, match="at least one channel"):
+        ssc.linear(torch.zeros(2, cin), torch.zeros(cout, cin))
