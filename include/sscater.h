@@ -443,7 +443,10 @@ int sscater_tokens_append(const sscater_head_spec* spec, const sscater_token_cac
  * [head_dim], as q; q and out on 16-byte boundaries.  window >= 1; q_heads a
  * multiple of kv_heads.  The keys in reach must still be held: capacity - sinks
  * at least min(window + max_new - 1, max_past + max_new), else
- * SSCATER_E_INVALID_ARG. */
+ * SSCATER_E_INVALID_ARG.  Scores, maxima and sums are fp32.  bf16: probabilities
+ * are rounded to bf16 for their product with the values where a sequence may
+ * bring more than 32 rows (max_new * q_heads / kv_heads); up to 32 they keep 16
+ * bits. */
 typedef struct {
     int32_t q_heads, window, causal;
     float scale;

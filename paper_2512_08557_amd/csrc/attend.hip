@@ -14,9 +14,16 @@
 // sum are one value per lane; O^T = V^T P^T then takes those scores as its
 // second operand from the same registers: the keys of a matrix instruction may
 // come in any order as long as V's come in the same one.  V is read from LDS
-// with the transposing read (bf16).  exp is taken to base 2, sums in fp32;
-// probabilities are rounded to bf16 for the product with bf16 values (as large
-// as the output's own rounding), their sum is not.
+// with the transposing read (bf16).  exp is taken to base 2, sums in fp32.
+//
+// The product with bf16 values takes the probabilities in bf16.  Up to 32 rows
+// of a key head are bound by the cache's bytes and take them in two parts, which
+// hold 16 bits (one token of sixteen streams over 65536 keys 358 us, with one part
+// 358; eight tokens over 16384 keys 27.5, 26.9): the error is that of the output's
+// rounding alone.  More rows are bound by the products and take one part, an error
+// as large as the output's rounding (a window of 33480 tokens 1920 us, in two
+// parts 2680; 48 rows over 16384 keys 30.9 and 33.1).  The sum is of the
+// unrounded probabilities.
 //
 // WM of the four wavefronts share keys and take different rows, the other
 // 4 / WM groups take other tiles of keys and are joined at the end.  Where the
@@ -55,6 +62,7 @@ struct AttendShape {
     // split once per workgroup on their way into LDS, through registers.
     static constexpr bool PL = F32 && WM == 4;
     static constexpr int NP = PL ? 3 : 1;          // planes
+    static constexpr int PP = PL ? 3 : !F32 && WM == 1 ? 2 : 1;   // parts of a probability
     static constexpr int LRB = PL ? D * 2 : RB;    // bytes of a row in LDS
     static constexpr int CPR = LRB / 16;           // its 16-byte pieces
     static constexpr bool B16 = !F32 || PL;        // bf16 operands
@@ -404,7 +412,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                 for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
         }
         const float ms = m == -INFINITY ? 0.f : m;
-        uint4 pf[C::NT * 2][C::NP];                    // bf16 operands: eight probabilities each
+        uint4 pf[C::NT * 2][C::PP];                    // bf16 operands: eight probabilities each
         // the values of 16 keys (bf16 operands) or of two (fp32), all of a head
         constexpr int VS = C::B16 ? C::BN / 16 : 16, VA = C::B16 ? 2 : 4;
         Operand vf[VA][D / 32];
@@ -450,8 +458,11 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                         cut_pair(__float_as_uint(s[e >> 4][(e & 15) - 1]), __float_as_uint(x), w[0], w[1], w[2]);
                     else
                         w[0] = bf16_pair(s[e >> 4][(e & 15) - 1], x);
+                    if constexpr (C::PP == 2)
+                        w[1] = bf16_pair(s[e >> 4][(e & 15) - 1] - __uint_as_float(w[0] << 16),
+                                         x - __uint_as_float(w[0] & 0xFFFF0000u));
 #pragma unroll
-                    for (int p = 0; p < C::NP; ++p) {
+                    for (int p = 0; p < C::PP; ++p) {
                         uint4& f = pf[e >> 3][p];
                         if ((e & 7) == 1) f.x = w[p];
                         else if ((e & 7) == 3) f.y = w[p];
@@ -470,6 +481,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
 #pragma unroll
             for (int t = 0; t < D / 32; ++t) {
                 const Operand& v = vf[ks % VA][t];
+                if constexpr (C::PP == 2) o[t] = mfma32(v.p[0], pf[ks][1], o[t]);
                 if constexpr (C::PL) o[t] = mfma_planes(v.p, pf[ks], o[t]);
                 else if constexpr (F32)
                     o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v.p[0].x), s[0][ks], o[t], 0, 0, 0);

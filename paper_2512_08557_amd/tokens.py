@@ -264,7 +264,9 @@ class TokenCache:
         keys and values appended, past not yet advanced) over the cache: a token
         sees the `window` newest tokens up to itself and the sinks (causal), or
         every new token of its stream and the window before them (not causal).
-        scale: 1 / sqrt(head_dim) unless given."""
+        scale: 1 / sqrt(head_dim) unless given.  bfloat16: where a stream may
+        bring more than 32 rows (max_new * q_heads / kv_heads) probabilities are
+        rounded to bfloat16 for the product with the values."""
         index = self.index
         _require(q, "q", self.kind, index)
         if q.dim() != 3 or q.shape[2] != self.head_dim or q.shape[1] < 1 or q.shape[1] % self.kv_heads:
