@@ -93,6 +93,9 @@ struct AttendShape {
     }
 };
 
+// What a copy reads for a group without a tile.
+__device__ __attribute__((aligned(16))) uint32_t attend_zero[4];
+
 // What a tile of rows reaches.
 struct Reach {
     int total;             // positions u
@@ -296,6 +299,11 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         if (WM > 1) lds_barrier();
         else asm volatile("" ::: "memory");
     };
+    // zeros in the place of a tile of values, for a group that goes round without one
+    auto no_values = [&](lds_char* to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < C::NC; ++j) copy16(attend_zero, to + (j * WM + wm) * 1024);
+    };
     lds_char* const kbuf = own;
     lds_char* const vbuf = own + 2 * C::TB;
 
@@ -345,12 +353,16 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         if (j + 1 < mine) {
             if constexpr (C::PL) fetch(tile_of(j + 1), vg, gv);
             else copy(tile_of(j + 1), vg, std::true_type{}, vbuf + (1 - P) * C::TB);
+        } else if (WM == 2 && j + 1 < rounds) {
+            no_values(vbuf + (1 - P) * C::TB);
         }
         const lds_char* kl = kbuf + (1 - P) * C::TB;
         const lds_char* vl = vbuf + P * C::TB;
         const int u0 = tile_of(j) * C::BN;
         clear(n);
-        // a tile that the wavefront does not see at all goes the same way (skipping it cost registers, and it spilled)
+        // A tile that the wavefront does not see at all goes the same way (skipping it cost registers, and it spilled), and
+        // so does the round in which a group has none: whatever its scores are they are left out, and its values are zeros
+        // (what the buffer held before must not be looked at: it would decide on `again`).
         const bool masked = j >= mine || u0 + C::BN - 1 > wl_first || (u0 < wf_last && u0 + C::BN > a.sinks);
         if (masked) {
 #pragma unroll
@@ -513,6 +525,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     };
     if (mine > 0) first_copy(tile_of(0), kg, std::false_type{}, kbuf);
     meet();
+    if (WM == 2 && mine == 0 && rounds > 0) no_values(vbuf);
     if (mine > 0) {
         first_copy(tile_of(0), vg, std::true_type{}, vbuf);
         if (mine > 1) first_copy(tile_of(1), kg, std::false_type{}, kbuf + C::TB);
