@@ -411,10 +411,11 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
             mx = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])) * a.scale;
         }
         // m is the reference of the row's exponents: a probability may be up to 2^8
-        // before it moves, so that the sums are hardly ever scaled again
+        // before it moves, so that the sums are hardly ever scaled again.  Rows that
+        // need not move keep theirs (scaled by 1): their bits are not the others' concern.
         if (__ballot(mx > m + 8.f) != 0) {
             asm volatile("");                          // a branch: the compiler would scale by 1 instead
-            const float mn = fmaxf(m, mx);
+            const float mn = mx > m + 8.f ? mx : m;
             const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.f : mn));
             m = mn;
             l *= alpha;

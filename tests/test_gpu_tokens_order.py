@@ -54,3 +54,23 @@ def test_results_do_not_depend_on_what_ran_before(kind, dim, rows, keys):
     for value in (math.inf, math.nan, -math.inf, 2.0 ** 100):
         leave(value)
         assert torch.equal(c.attend(q, keys), want), f"after a kernel over {value}"
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kind,dim,new,heads", [("bf16", 64, 1, 8), ("bf16", 64, 12, 4), ("bf16", 128, 50, 4),
+                                                ("bf16", 32, 200, 1), ("f32", 64, 12, 2), ("f32", 64, 40, 1),
+                                                ("f32", 32, 200, 2), ("f32", 128, 8, 4)])
+def test_a_row_does_not_depend_on_the_other_rows(kind, dim, new, heads, causal):
+    """A query forty times as large moves its own row's exponents and no other
+    row's bits."""
+    note(f"[gpu-test] other rows {kind} dim {dim} new {new} heads {heads} causal {causal}")
+    rng = np.random.default_rng(new * 10 + heads)
+    c = filled(rng, kind, 1, dim, 900, 700)
+    q = normal(rng, (new, heads, dim), KIND[kind], 2.0)
+    want = c.attend(q, 600, causal=causal)
+    for t, h in {(0, 0), (new // 2, heads - 1), (new - 1, 0)}:
+        other = q.clone()
+        other[t, h] *= 40
+        got = c.attend(other, 600, causal=causal)
+        got[t, h] = want[t, h]
+        assert torch.equal(got, want), f"query {t}, {h}"
