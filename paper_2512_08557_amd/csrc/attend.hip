@@ -33,6 +33,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <limits>
 #include <type_traits>
 
 namespace ssc {
@@ -807,7 +808,8 @@ int sscater_tokens_attend(const sscater_attend_spec* spec, const sscater_token_c
     a.q_heads = spec->q_heads; a.kv_heads = cache->kv_heads; a.group = spec->q_heads / cache->kv_heads;
     a.sinks = cache->sinks; a.capacity = cache->capacity; a.window = spec->window; a.causal = spec->causal;
     a.qtiles = cut.qtiles; a.splits = cut.splits;
-    a.scale = std::max(std::fabs(spec->scale) * 1.4426950408889634f, 1e-30f);   // times -inf it stays that
+    // not zero, so that a masked score times it stays -inf; the least number of all, times a finite score, is zero beside 1
+    a.scale = std::max(std::fabs(spec->scale) * 1.4426950408889634f, std::numeric_limits<float>::denorm_min());
     a.flip = spec->scale < 0.f ? cache->dtype == SSCATER_F32 ? 0x80000000u : 0x80008000u : 0u;
     if (cache->dtype == SSCATER_F32) launch_attend<true>(a, cut, cache->head_dim, (hipStream_t)stream);
     else launch_attend<false>(a, cut, cache->head_dim, (hipStream_t)stream);

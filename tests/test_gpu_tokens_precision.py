@@ -52,3 +52,27 @@ def test_single_bf16_tokens_are_off_by_the_rounding_of_the_output_alone(batch, h
             worst = max(worst, float(((got[b, h] - ref).abs() / tol).max()))
     note(f"[gpu-test] {worst:.3f} of the tolerance")
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [1, 40, 150])
+@pytest.mark.parametrize("scale", [1e-32, 0.0, -1e-32])
+def test_tiny_scales(kind, new, scale):
+    """Scores whose scale is far below one and whose products are as large.
+    Tolerance: as for attention in general, 2^-8 for every bf16 probability and
+    the output."""
+    note(f"[gpu-test] scale {scale} {kind} new {new}")
+    rng = np.random.default_rng(new)
+    dtype = torch.float32 if kind == "f32" else torch.bfloat16
+    k, v = normal(rng, (1, 1, 200, 32), dtype, 1e16), normal(rng, (1, 1, 200, 32), dtype)
+    c = ssc.TokenCache(1, 1, 32, 200, dtype=kind, k=k, v=v)
+    c.seek([200 - new])
+    q = normal(rng, (new, 1, 32), dtype, 1e15)
+    got = c.attend(q, 200, causal=False, scale=scale)[:, 0].double().cpu()
+    q, k, v = q[:, 0].double().cpu(), k[0, 0].double().cpu(), v[0, 0].double().cpu()
+    s = scale * (q @ k.t())
+    p = torch.softmax(s, -1)
+    err = 2 * (math.sqrt(32) + 8) * U * abs(scale) * (q.abs() @ k.abs().t()) + 4 * U * s.abs()
+    rel = 2 * err.max(-1, keepdim=True)[0] + 2 * (math.sqrt(200) + 8) * U + (2.0 ** -8 if kind == "bf16" else 0)
+    tol = rel * (p @ v.abs()) + (2.0 ** -8 * (kind == "bf16") + 2 * U) * (p @ v).abs()
+    assert bool(((got - p @ v).abs() <= tol).all()), float(((got - p @ v).abs() / tol).max())
