@@ -352,7 +352,7 @@ int sscater_profile_read(sscater_t h, double* ms, int64_t* launches, int32_t n, 
 typedef enum {
     SSCATER_ACT_NONE = 0,
     SSCATER_ACT_RELU = 1, /* max(z, 0); NaN stays NaN */
-    SSCATER_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2 */
+    SSCATER_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2, within 4 * 2^-24 |z|; 0 at minus infinity */
     SSCATER_ACT_SILU = 3  /* z / (1 + exp(-z)) */
 } sscater_activation;
 

@@ -76,3 +76,34 @@ def test_tiny_scales(kind, new, scale):
     rel = 2 * err.max(-1, keepdim=True)[0] + 2 * (math.sqrt(200) + 8) * U + (2.0 ** -8 if kind == "bf16" else 0)
     tol = rel * (p @ v.abs()) + (2.0 ** -8 * (kind == "bf16") + 2 * U) * (p @ v).abs()
     assert bool(((got - p @ v).abs() <= tol).all()), float(((got - p @ v).abs() / tol).max())
+
+
+@pytest.mark.parametrize("rows", [50, 20000])
+def test_gelu_tends_to_zero(rows):
+    """z Phi(z) of z = x (one channel, weight 1).  Everywhere within 4 u |z| (the
+    polynomial 1.7e-8, its evaluation and the exponential 2.5 u, the sum u); from
+    z = -6 downwards no further from zero than a tenth above the function itself
+    (the polynomial lies below log2 Phi there), and zero at minus infinity."""
+    note(f"[gpu-test] gelu tail {rows}")
+    z = torch.linspace(-45, 12, rows)
+    z[0], z[1], z[-1], z[2] = -math.inf, -3e38, math.inf, -1000.0
+    y = ssc.linear(z[:, None].cuda(), torch.ones(1, 1, device="cuda"), activation="gelu")[:, 0].double().cpu()
+    assert y[0] == 0 and y[1] == 0 and y[2] == 0 and y[-1] == math.inf
+    z, y = z.double()[3:-1], y[3:-1]
+    ref = 0.5 * z * torch.special.erfc(-z / math.sqrt(2))
+    assert bool(((y - ref).abs() <= 4 * U * z.abs() + 1e-45).all()), float(((y - ref).abs() / (4 * U * z.abs())).max())
+    tail = z <= -6
+    assert bool((y[tail].abs() <= 1.1 * ref[tail].abs()).all()), float((y[tail] / ref[tail]).abs().max())
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [20, 20000])
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_activations_keep_nan_and_infinity(act, rows, kind):
+    dtype = torch.float32 if kind == "f32" else torch.bfloat16
+    x = torch.ones(rows, 8, dtype=dtype, device="cuda")
+    x[1, 2], x[rows - 1, 0], x[3, 1] = math.nan, math.nan, math.inf
+    y = ssc.linear(x, torch.ones(128, 8, dtype=dtype, device="cuda"), activation=act)
+    lost = torch.isnan(y).all(1).cpu()
+    assert lost[1] and lost[rows - 1] and int(lost.sum()) == 2 and int(torch.isnan(y).sum()) == 256
+    assert bool((y[3] == math.inf).all()) and int(torch.isinf(y).sum()) == 128
