@@ -382,6 +382,10 @@ __device__ __forceinline__ void cut_pair(uint32_t x, uint32_t y, uint32_t& h, ui
 
 typedef float f16v __attribute__((ext_vector_type(16)));
 
+// Workgroups of 256 threads that one launch gets at most: HIP takes fewer than
+// 2^32 threads, larger calls are several launches.
+constexpr int64_t LAUNCH_GROUPS = 1 << 23;
+
 __device__ __forceinline__ f16v mfma32(uint4 a, uint4 b, f16v c) {
     bf8v A, B;
     __builtin_memcpy(&A, &a, 16);

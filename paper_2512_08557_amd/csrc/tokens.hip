@@ -32,6 +32,7 @@ struct AppendArgs {
     int q_heads, kv_heads, axes, sinks, capacity, even;
     int end0, end1;        // pairs of the first axis, and of the first two
     int tt;                // tokens of a workgroup
+    int token0;            // first token of the launch
     float eps;
 };
 
@@ -76,7 +77,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
     constexpr int G = D / (2 * E);                   // lanes of a head
     __shared__ float2 turn[APPEND_TOKENS][D / 2];
     __shared__ int64_t slot[APPEND_TOKENS];           // cache row of the token's first head, or -1
-    const int t0 = blockIdx.x * a.tt;
+    const int t0 = a.token0 + (int)blockIdx.x * a.tt;
     const int nt = min(a.tt, a.rows.tokens - t0);
     for (int i = threadIdx.x; i < nt * (D / 2); i += 256) {
         const int t = i / (D / 2), p = i % (D / 2);
@@ -221,10 +222,13 @@ TokenRows token_rows(const sscater_token_cache* c, const sscater_token_rows* r) 
 namespace {
 
 template <bool F32, int D>
-void launch_append(const AppendArgs& a, bool vec, hipStream_t s) {
-    const dim3 grid((a.rows.tokens + a.tt - 1) / a.tt), block(256);
-    if (vec) append_kernel<F32, D, true><<<grid, block, 0, s>>>(a);
-    else append_kernel<F32, D, false><<<grid, block, 0, s>>>(a);
+void launch_append(AppendArgs a, bool vec, hipStream_t s) {
+    for (int64_t t = 0; t < a.rows.tokens; t += LAUNCH_GROUPS * a.tt) {
+        a.token0 = (int)t;
+        const dim3 grid((unsigned)std::min(LAUNCH_GROUPS, (a.rows.tokens - t + a.tt - 1) / a.tt)), block(256);
+        if (vec) append_kernel<F32, D, true><<<grid, block, 0, s>>>(a);
+        else append_kernel<F32, D, false><<<grid, block, 0, s>>>(a);
+    }
 }
 
 template <bool F32>
