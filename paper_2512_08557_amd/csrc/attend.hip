@@ -50,6 +50,7 @@ struct AttendArgs {
     int q_heads, kv_heads, group;
     int sinks, capacity, window, causal;
     int qtiles, splits;
+    int id0;               // first workgroup of the launch
     float scale;           // its size times log2(e)
     uint32_t flip;         // sign bits of the queries, flipped for a negative scale
 };
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     // its L2; the last tokens' tiles, which reach furthest, come first, and short ones fill up the end.  Of few rows
     // nothing is read twice: there splits go fastest, and every XCD has a part of each sequence, long or short (16 ragged
     // streams over 65536 keys 190 us, with key heads fastest 215).
-    int id = blockIdx.x, kvh, b, split, tile;
+    int id = a.id0 + (int)blockIdx.x, kvh, b, split, tile;
     if constexpr (WM == 1) {
         split = id % a.splits;
         id /= a.splits;
@@ -757,14 +758,18 @@ size_t attend_bytes(const AttendCut& cut, const sscater_attend_spec* s, const ss
 }
 
 template <bool F32, int D>
-void launch_attend(const AttendArgs& a, const AttendCut& cut, hipStream_t s) {
-    const dim3 grid((unsigned)cut.grid), block(256);
-    if constexpr (!(F32 && D == 128)) {
-        if (cut.wm == 1) attend_kernel<F32, D, 1><<<grid, block, 0, s>>>(a);
+void launch_attend(AttendArgs a, const AttendCut& cut, hipStream_t s) {
+    const dim3 block(256);
+    for (int64_t at = 0; at < cut.grid; at += LAUNCH_GROUPS) {
+        a.id0 = (int)at;
+        const dim3 grid((unsigned)std::min(LAUNCH_GROUPS, cut.grid - at));
+        if constexpr (!(F32 && D == 128)) {
+            if (cut.wm == 1) attend_kernel<F32, D, 1><<<grid, block, 0, s>>>(a);
+        }
+        if (cut.wm == 2) attend_kernel<F32, D, 2><<<grid, block, 0, s>>>(a);
+        if (cut.wm == 4) attend_kernel<F32, D, 4><<<grid, block, 0, s>>>(a);
     }
-    if (cut.wm == 2) attend_kernel<F32, D, 2><<<grid, block, 0, s>>>(a);
-    if (cut.wm == 4) attend_kernel<F32, D, 4><<<grid, block, 0, s>>>(a);
-    if (cut.splits > 1) {
+    if (cut.splits > 1) {                              // at most some hundred thousand rows: see attend_cut
         const int64_t rows = (int64_t)a.rows.tokens * a.q_heads;
         join_kernel<F32, D><<<dim3((unsigned)((rows + 3) / 4)), block, 0, s>>>(a.part, a.out, rows, cut.splits);
     }

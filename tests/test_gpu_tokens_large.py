@@ -31,3 +31,13 @@ def test_append_of_many_tokens():
     assert torch.equal(c.k[0, 0, slot], qkv[held, dim:2 * dim]) and torch.equal(c.v[0, 0, slot], qkv[held, 2 * dim:])
     c.advance(tokens)
     assert c.past.tolist() == [tokens]
+
+
+def test_attention_of_many_streams():
+    """2^23 streams with one key each, two heads: the values themselves."""
+    batch = 1 << 23
+    note(f"[gpu-test] attend {batch}")
+    gen = torch.Generator("cuda").manual_seed(2)
+    make = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)  # noqa: E731
+    c = ssc.TokenCache(batch, 2, 32, 1, dtype="bf16", k=make(batch, 2, 1, 32), v=make(batch, 2, 1, 32))
+    assert torch.equal(c.attend(make(batch, 2, 32), 1), c.v[:, :, 0])
