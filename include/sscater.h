@@ -357,7 +357,8 @@ typedef enum {
 } sscater_activation;
 
 /* A linear layer over rows: y = act(x W^T + bias) + residual.
- *   rows >= 0, cin, cout >= 1; x [rows][cin], W [cout][cin] (a 1x1 convolution's
+ *   rows >= 0, cin, cout >= 1 (rows <= 2^36, cin, cout <= 2^30, rows * cout <=
+ *   2^40); x [rows][cin], W [cout][cin] (a 1x1 convolution's
  *   OIHW weights), bias [cout], residual and y [rows][cout], all in dtype;
  *   *_stride: elements between two rows, at least the row's length (ignored
  *   for a null residual). */
@@ -384,7 +385,8 @@ int sscater_linear(const sscater_linear_spec* spec, const void* x, const void* w
  * tokens a stream has seen.  Token j of a stream (j = 0 its first ever) sits in
  * slot j if j < sinks, else in slot sinks + (j - sinks) mod (capacity - sinks):
  * the first tokens stay, the others give way to the newest.
- *   head_dim 32, 64 or 128; 0 <= sinks < capacity. */
+ *   head_dim 32, 64 or 128; 0 <= sinks < capacity <= 2^30; batch <= 2^24,
+ *   kv_heads <= 2^16. */
 typedef struct {
     int32_t dtype; /* sscater_dtype */
     int32_t batch, kv_heads, head_dim;
@@ -397,7 +399,8 @@ typedef struct {
 /* The new tokens of a call: `tokens` rows, sequence b's being rows start[b] to
  * start[b + 1] - 1 (start: device int32[batch + 1], increasing from 0 to
  * tokens, or NULL: max_new rows each, tokens = batch * max_new).  max_new: the
- * most that one sequence brings; max_past: no less than any past[b]. */
+ * most that one sequence brings; max_past: no less than any past[b]; tokens <=
+ * 2^30, max_past <= 2^62. */
 typedef struct {
     int32_t tokens, max_new;
     int64_t max_past;
@@ -441,7 +444,7 @@ int sscater_tokens_append(const sscater_head_spec* spec, const sscater_token_cac
  *               another and the same past);
  * out = sum_j softmax_j(scale * q . k_j) v_j, device [tokens][q_heads]
  * [head_dim], as q; q and out on 16-byte boundaries.  window >= 1; q_heads a
- * multiple of kv_heads.  The keys in reach must still be held: capacity - sinks
+ * multiple of kv_heads, at most 2^16; max_new * q_heads / kv_heads <= 2^30.  The keys in reach must still be held: capacity - sinks
  * at least min(window + max_new - 1, max_past + max_new), else
  * SSCATER_E_INVALID_ARG.  Scores, maxima and sums are fp32.  bf16: probabilities
  * are rounded to bf16 for their product with the values where a sequence may

@@ -760,30 +760,24 @@ __global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a) {
 namespace {
 
 template <bool F32, bool VEC, int WM, int WN, int TM, int TN>
-bool launch_tiles(LinearArgs& a, hipStream_t s) {
+void launch_tiles(LinearArgs& a, hipStream_t s) {
     using C = LinearShape<F32, VEC, WM, WN, TM, TN>;
     a.tn = (a.N + C::BN - 1) / C::BN;
-    const int64_t tiles = (a.M + C::BM - 1) / C::BM * a.tn;
-    if (tiles > 0x7FFFFFF0) return false;
-    a.tiles = (int)tiles;
-    a.per_xcd = (int)((tiles + 7) / 8);
+    a.tiles = (int)((a.M + C::BM - 1) / C::BM * a.tn);
+    a.per_xcd = (a.tiles + 7) / 8;
     a.packed = a.tn == 1 && a.ldy == a.N && (uintptr_t)a.y % 16 == 0;
     linear_kernel<F32, VEC, WM, WN, TM, TN><<<dim3((unsigned)a.per_xcd * 8), dim3(256), 0, s>>>(a);
-    return true;
 }
 
-bool launch_big(LinearArgs& a, hipStream_t s) {
+void launch_big(LinearArgs& a, hipStream_t s) {
     a.tn = (a.N + BigShape::BN - 1) / BigShape::BN;
-    const int64_t tiles = (a.M + BigShape::BM - 1) / BigShape::BM * a.tn;
-    if (tiles > 0x7FFFFFF0) return false;
-    a.tiles = (int)tiles;
-    a.per_xcd = (int)((tiles + 7) / 8);
+    a.tiles = (int)((a.M + BigShape::BM - 1) / BigShape::BM * a.tn);
+    a.per_xcd = (a.tiles + 7) / 8;
     linear_big_kernel<<<dim3(256), dim3(512), 0, s>>>(a);
-    return true;
 }
 
 template <bool F32, bool VEC>
-bool launch_linear(LinearArgs& a, hipStream_t s) {
+void launch_linear(LinearArgs& a, hipStream_t s) {
     // Which kernel, by how many tiles there are for 256 compute units (us on either side of each bound):
     // fewer than 128 tiles of 64 x 64 leave units idle for all of K, so K is shared (500 x 512 -> 512 fp32, 64 tiles: rows
     // 9.8, tiles 17.0; 600 x 1024 -> 1024 bf16, 160 tiles: rows 13.6, tiles 10.4); the rows kernel's larger block from 512
@@ -796,7 +790,7 @@ bool launch_linear(LinearArgs& a, hipStream_t s) {
         const dim3 grid((unsigned)(one ? small : (a.M + 31) / 32 * n32));
         if (one) linear_rows_kernel<F32, VEC, 1><<<grid, dim3(256), 0, s>>>(a);
         else linear_rows_kernel<F32, VEC, 2><<<grid, dim3(256), 0, s>>>(a);
-        return true;
+        return;
     }
     // the persistent kernel where its passes over the card are nearly full (53568 x 384 -> 384, 630 of 768 places: 29.3,
     // tiles of 128 31.9; 24000 x 256 -> 512, 376 of 512: 23.5 and 17.7), a little less so for a long K (8192 x 1536 ->
@@ -812,6 +806,27 @@ bool launch_linear(LinearArgs& a, hipStream_t s) {
     // 43.8; 12000 x 1024 -> 256 fp32, 188: 63.7 and 50.7)
     if (a.N > 64 && (a.M + 127) / 128 * ((a.N + 127) / 128) >= 400) return launch_tiles<F32, VEC, 2, 2, 2, 2>(a, s);
     return launch_tiles<F32, VEC, 2, 2, 1, 1>(a, s);
+}
+
+// Parts of a call that are one launch each: at most 2^22 channels, and rows whose
+// smallest tiles (64 x 64) are no more than LAUNCH_GROUPS.  All but the last have
+// rows and channels in multiples of 256, so that they keep the call's alignment.
+template <bool F32, bool VEC>
+void launch_parts(const LinearArgs& all, hipStream_t s) {
+    constexpr int64_t SIZE = F32 ? 4 : 2, CHANNELS = 1 << 22;
+    const int64_t tn = (std::min((int64_t)all.N, CHANNELS) + 63) / 64, rows = 64 * (LAUNCH_GROUPS / tn & ~int64_t(3));
+    for (int64_t n = 0; n < all.N; n += CHANNELS)
+        for (int64_t m = 0; m < all.M; m += rows) {
+            LinearArgs a = all;
+            a.N = (int)std::min(CHANNELS, all.N - n);
+            a.M = std::min(rows, all.M - m);
+            a.x = (const char*)all.x + m * all.ldx * SIZE;
+            a.w = (const char*)all.w + n * all.ldw * SIZE;
+            a.bias = all.bias ? (const char*)all.bias + n * SIZE : nullptr;
+            a.res = all.res ? (const char*)all.res + (m * all.ldr + n) * SIZE : nullptr;
+            a.y = (char*)all.y + (m * all.ldy + n) * SIZE;
+            launch_linear<F32, VEC>(a, s);
+        }
 }
 
 }  // namespace
@@ -830,6 +845,7 @@ extern "C" int sscater_linear(const sscater_linear_spec* spec, const void* x, co
         (residual && spec->residual_stride < spec->cout))
         return SSCATER_E_INVALID_ARG;
     if (spec->rows == 0) return SSCATER_OK;
+    if (spec->cout > (int64_t(1) << 40) / spec->rows) return SSCATER_E_INVALID_ARG;
     const int size = spec->dtype == SSCATER_F32 ? 4 : 2;
     for (const void* p : {x, weight, (const void*)y})
         if (!p || (uintptr_t)p % size) return SSCATER_E_INVALID_ARG;
@@ -846,9 +862,8 @@ extern "C" int sscater_linear(const sscater_linear_spec* spec, const void* x, co
     a.yvec = (uintptr_t)y % 16 == 0 && a.ldy % per == 0;
     a.rvec = (uintptr_t)residual % 16 == 0 && a.ldr % per == 0;
     const hipStream_t s = (hipStream_t)stream;
-    const bool fits = size == 4 ? vec ? launch_linear<true, true>(a, s) : launch_linear<true, false>(a, s)
-                                : vec ? launch_linear<false, true>(a, s) : launch_linear<false, false>(a, s);
-    if (!fits) return SSCATER_E_INVALID_ARG;
+    if (size == 4) vec ? launch_parts<true, true>(a, s) : launch_parts<true, false>(a, s);
+    else vec ? launch_parts<false, true>(a, s) : launch_parts<false, false>(a, s);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SSCATER_OK : report_hip_error(e);
 }

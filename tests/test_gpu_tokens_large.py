@@ -41,3 +41,27 @@ def test_attention_of_many_streams():
     make = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)  # noqa: E731
     c = ssc.TokenCache(batch, 2, 32, 1, dtype="bf16", k=make(batch, 2, 1, 32), v=make(batch, 2, 1, 32))
     assert torch.equal(c.attend(make(batch, 2, 32), 1), c.v[:, :, 0])
+
+
+def test_linear_over_many_rows():
+    """2^31 + 300 rows of one channel: one product each, rounded once."""
+    rows, part = (1 << 31) + 300, 1 << 28
+    note(f"[gpu-test] linear {rows}")
+    gen = torch.Generator("cuda").manual_seed(3)
+    x = torch.empty(rows, 1, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    w = torch.full((1, 1), 1.3, dtype=torch.bfloat16, device="cuda")
+    y = ssc.linear(x, w)
+    for i in range(0, rows, part):
+        assert torch.equal(y[i:i + part], (x[i:i + part].float() * w.float()).to(torch.bfloat16)), i
+
+
+def test_linear_over_many_channels():
+    """2^24 channels of a few rows, in parts of the layer: products, biases and
+    residuals (whole numbers, so every sum is exact) meet their own."""
+    channels = (1 << 24) + 72
+    note(f"[gpu-test] linear to {channels}")
+    i = torch.arange(channels, device="cuda")
+    x = torch.arange(1, 71, device="cuda").float()[:, None]
+    w, b = (i * 37 % 251 - 125).float()[:, None], (i * 11 % 1009).float()
+    r = (torch.arange(70 * channels, device="cuda").view(70, channels) * 7 % 2003).float()
+    assert torch.equal(ssc.linear(x, w, b, residual=r), x * w.t() + b + r)
