@@ -24,11 +24,13 @@ _KINDS: dict = {}
 
 def _bind():
     """torch, at the first call (as in Engine), and its current device and
-    stream as plain numbers: the objects around them cost more than a launch."""
+    stream as plain numbers: the objects around them cost more than a launch.
+    torch comes last: callers on other threads take it for a sign of the rest."""
     global torch, _device, _stream
     import torch as t
-    torch, _device, _stream = t, t._C._cuda_getDevice, t._C._cuda_getCurrentRawStream
     _KINDS.update({t.float32: F32, t.bfloat16: BF16})
+    _device, _stream = t._C._cuda_getDevice, t._C._cuda_getCurrentRawStream
+    torch = t
 
 
 def _require(t, name: str, dtype, index: int, shape=None):
