@@ -1,5 +1,6 @@
 """Token operators of libsscater.so: linear layers over rows of cells, and
-attention over the tokens of earlier strides (argument marshalling only).
+attention over the tokens of earlier strides (argument marshalling only).  They
+form no gradients: where one would be wanted they refuse the call.
 
 As in engine.py, tensors give device pointers and the HIP stream is torch's
 current one unless another is passed; every value is computed in the library's
@@ -50,6 +51,13 @@ def _dense(t, name: str, dtype, index: int, shape):
     if not _require(t, name, dtype, index, shape).is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+def _want_gradient() -> None:
+    """Called for operands that require a gradient: a result without one would be
+    taken for a constant."""
+    if torch.is_grad_enabled():
+        raise ValueError("no gradient is formed: detach the operands or call under torch.no_grad()")
 
 
 def _launch(fn, where: str, index: int, stream, tensors, *args) -> None:
@@ -128,6 +136,9 @@ def linear(x, weight, bias=None, activation: Optional[str] = None, residual=None
             raise ValueError("bias must be contiguous")
     if residual is not None:
         rs = _row_stride(_require(residual, "residual", dtype, index, shape), "residual", cout)
+    if x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad) or \
+            (residual is not None and residual.requires_grad):
+        _want_gradient()
     if out is None:
         out, ys = x.new_empty(shape), cout
     else:
@@ -248,6 +259,10 @@ class TokenCache:
         qw = kw = None
         if q_weight is not None:
             qw, kw = (_dense(w, "q_weight and k_weight", self.kind, index, (dim,)) for w in (q_weight, k_weight))
+            if q_weight.requires_grad or k_weight.requires_grad:
+                _want_gradient()
+        if qkv.requires_grad:
+            _want_gradient()
         rows = self._rows(tokens, start, max_new)
         shape = (tokens, q_heads, dim)
         if out is None:
@@ -277,6 +292,8 @@ class TokenCache:
             raise ValueError("q must be contiguous, on a 16-byte boundary")
         if window < 1:
             raise ValueError("window must be at least 1")
+        if q.requires_grad:
+            _want_gradient()
         rows = self._rows(q.shape[0], start, max_new)
         if out is None:
             out = q.new_empty(q.shape)
