@@ -43,7 +43,7 @@ class TemporalBlock:
         self.weights = dict(weights)
         self.q_heads, self.batch = int(q_heads), int(batch)
         # a stride's tokens and the ones before them
-        self.window = strides * tokens + 1
+        self.window, self.tokens = strides * tokens + 1, int(tokens)
         dtype = "f32" if weights["qkv"].dtype == torch.float32 else "bf16"
         device = weights["qkv"].device
         self.cache = TokenCache(batch, kv_heads, head_dim, sinks + self.window + tokens - 1, sinks=sinks, dtype=dtype,
@@ -65,8 +65,12 @@ class TemporalBlock:
         return self._pos
 
     def step(self, x, stride: int, grid: Tuple[int, int]):
-        """One stride's cells x [batch * H * W, C]; the result has their shape."""
+        """One stride's cells x [batch * H * W, C], at most `tokens` of a map; the
+        result has their shape."""
         w, n = self.weights, x.shape[0]
+        # before anything is put into the cache, where more of them would go over tokens that are still looked back at
+        if grid[0] * grid[1] > self.tokens:
+            raise ValueError(f"a map of {grid[0]} x {grid[1]} cells: a stride brings at most {self.tokens}")
         qkv = linear(x, w["qkv"], w.get("qkv_bias"))
         q = self.cache.append(qkv, self.positions(stride, grid), self.rotary, self.q_heads, q_weight=w["q_norm"],
                               k_weight=w["k_norm"])

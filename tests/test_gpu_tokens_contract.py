@@ -1,4 +1,5 @@
 """GPU tests of which calls the token operators refuse, and of what a refused one leaves."""
+import numpy as np
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -36,3 +37,17 @@ def test_operands_that_want_a_gradient_are_refused():
         c.attend(q.clone().requires_grad_(), 4)
     with torch.no_grad():
         assert torch.equal(c.attend(q.clone().requires_grad_(), 4), c.attend(q, 4))
+
+
+def test_a_stride_of_too_many_cells_leaves_the_block_as_it_was():
+    rng = np.random.default_rng(3)
+    make = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32) * s[-1] ** -0.5).cuda()  # noqa: E731
+    w = {"qkv": make(3 * 64, 32), "q_norm": torch.ones(32).cuda(), "k_norm": torch.ones(32).cuda(),
+         "out": make(32, 64), "up": make(96, 32), "down": make(32, 96)}
+    one, two = (ssc.TemporalBlock(w, 2, 2, 32, tokens=9, strides=2, sinks=1) for _ in range(2))
+    for stride in range(8):
+        x = make(9, 32)
+        if stride in (0, 5):
+            with pytest.raises(ValueError, match="9"):
+                two.step(make(16, 32), stride, (4, 4))
+        assert torch.equal(one.step(x, stride, (3, 3)), two.step(x, stride, (3, 3))), f"stride {stride}"
