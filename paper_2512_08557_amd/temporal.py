@@ -21,6 +21,7 @@ from typing import Dict, Optional, Sequence, Tuple
 from .tokens import Rotary, TokenCache, linear
 
 NAMES = ("qkv", "q_norm", "k_norm", "out", "up", "down")
+BIASES = ("qkv_bias", "out_bias", "up_bias", "down_bias")
 
 
 class TemporalBlock:
@@ -44,7 +45,12 @@ class TemporalBlock:
         self.q_heads, self.batch = int(q_heads), int(batch)
         # a stride's tokens and the ones before them
         self.window, self.tokens = strides * tokens + 1, int(tokens)
-        dtype = "f32" if weights["qkv"].dtype == torch.float32 else "bf16"
+        dtype = {torch.float32: "f32", torch.bfloat16: "bf16"}.get(weights["qkv"].dtype)
+        if dtype is None:
+            raise ValueError(f"weights must be float32 or bfloat16, not {weights['qkv'].dtype}")
+        other = [n for n in NAMES + BIASES if weights.get(n) is not None and weights[n].dtype != weights["qkv"].dtype]
+        if other:
+            raise ValueError(f"weights of one dtype: {other} differ from qkv")
         device = weights["qkv"].device
         self.cache = TokenCache(batch, kv_heads, head_dim, sinks + self.window + tokens - 1, sinks=sinks, dtype=dtype,
                                 device=device)
