@@ -800,8 +800,10 @@ void launch_linear(LinearArgs& a, hipStream_t s) {
         const int64_t places = (tiles + 255) / 256 * 256;
         if (a.N > 64 && (tiles * 5 >= places * 4 || (tiles * 10 >= places * 7 && a.K >= 1024))) return launch_big(a, s);
     }
-    // a tile of all channels, unless rows of exactly 64 can be stored as they are
-    if (a.N <= 64 && !(a.N == 64 && a.yvec) && a.M >= 256 * 64) return launch_tiles<F32, VEC, 4, 1, 1, 2>(a, s);
+    // a tile of all channels, unless rows of exactly 64 can be stored as they are, once there is one for every compute unit
+    // (384 -> 42 bf16: 16384 rows 9.1, tiles of 64 x 64 8.4; 32768: 10.8 and 10.9; 53568: 11.7 and 15.6; 256 -> 42 fp32:
+    // 14.1 and 11.1, 14.7 and 13.9, 17.5 and 20.7)
+    if (a.N <= 64 && !(a.N == 64 && a.yvec) && a.M >= 256 * 128) return launch_tiles<F32, VEC, 4, 1, 1, 2>(a, s);
     // 128 x 128 from 400 of them on (12000 x 256 -> 512 bf16, 376: 13.4, 64 x 64 10.1; 30000 x 1536 -> 256, 470: 33.2 and
     // 43.8; 12000 x 1024 -> 256 fp32, 188: 63.7 and 50.7)
     if (a.N > 64 && (a.M + 127) / 128 * ((a.N + 127) / 128) >= 400) return launch_tiles<F32, VEC, 2, 2, 2, 2>(a, s);
