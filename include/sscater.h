@@ -371,9 +371,10 @@ typedef struct {
 } sscater_linear_spec;
 
 /* bias and residual may be NULL.  y may be the residual itself (same pointer
- * and stride) and must not overlap x, W or bias.  Sums are fp32; fp32 products
- * are formed from three bf16 parts of either factor, which hold its 24 bits;
- * bf16 outputs are rounded once.  A row may be aligned to its elements only;
+ * and stride) and must not overlap x, W or bias.  Sums are fp32.  fp32 products
+ * over many rows are formed from three bf16 parts of either factor, which hold
+ * its 24 bits (but for those below 2^-133), and are at most 2^-21 of themselves
+ * off, towards zero.  bf16 outputs are rounded once.  A row may be aligned to its elements only;
  * rows of x and W that are multiples of 16 bytes apart and start on one are
  * read faster. */
 int sscater_linear(const sscater_linear_spec* spec, const void* x, const void* weight, const void* bias,
@@ -449,7 +450,8 @@ int sscater_tokens_append(const sscater_head_spec* spec, const sscater_token_cac
  * SSCATER_E_INVALID_ARG.  Scores, maxima and sums are fp32.  bf16: probabilities
  * are rounded to bf16 for their product with the values where a sequence may
  * bring more than 32 rows (max_new * q_heads / kv_heads); up to 32 they keep 16
- * bits. */
+ * bits.  Sums are divided at the end and hold probabilities up to 2^8: they may
+ * overflow for values beyond 2^119 divided by the keys in reach. */
 typedef struct {
     int32_t q_heads, window, causal;
     float scale;

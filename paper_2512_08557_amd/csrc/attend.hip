@@ -149,8 +149,8 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     const int h = lane >> 5, col = lane & 31;
     // Key heads go fastest, so that an XCD (workgroup id mod 8) keeps to one or a few of them and finds their keys in
     // its L2; the last tokens' tiles, which reach furthest, come first, and short ones fill up the end.  Of few rows
-    // nothing is read twice: there splits go fastest, and every XCD has a part of each sequence, long or short (16 ragged
-    // streams over 65536 keys 190 us, with key heads fastest 215).
+    // nothing is read twice: there splits go fastest, and every XCD has a part of each sequence, long or short (nine
+    // streams of different lengths over up to 65536 keys 190 us, with key heads fastest 215).
     int id = a.id0 + (int)blockIdx.x, kvh, b, split, tile;
     if constexpr (WM == 1) {
         split = id % a.splits;
@@ -695,7 +695,8 @@ __global__ __launch_bounds__(256) void join_kernel(const float* part, void* out,
 
 namespace {
 
-// Workgroups of attend_kernel that a compute unit takes.
+// Workgroups of attend_kernel that a compute unit is asked to take (the launch bounds).  Registers and LDS leave room
+// for more in places: two of fp32 heads of 64 with WM 2 and 4, three or four of heads of 32.
 template <bool F32, int D>
 int attend_places(int wm) {
     if constexpr (!(F32 && D == 128))

@@ -4,17 +4,19 @@
 // consecutive output channels of one row; sums are fp32, rounded once.  Four
 // kernels, by the number of rows and channels:
 //   few rows      linear_rows_kernel: K shared by the wavefronts, no LDS on the way
-//                 in (4 x 256 -> 1024 bf16: 3.0 us, a launch and two round trips);
+//                 in (4 x 256 -> 1024 bf16: 2.9 us, a launch and two round trips);
 //   some rows     linear_kernel: tiles of 64 x 64, 128 x 128 or 128 x 64 through LDS
-//                 (12000 x 1024 -> 256 fp32 with residual 48 us, 132 TFLOP/s; a head of
-//                 42 channels over 53568 x 384 bf16 11.7 us, 3.9 TB/s);
+//                 (12000 x 1024 -> 256 fp32 with residual 49 us, 127 TFLOP/s; a head of
+//                 42 channels over 53568 x 384 bf16 11.6 us, 4.0 TB/s);
 //   many, in bf16 linear_big_kernel: persistent tiles of 256 x 128
-//                 (214272 x 384 -> 1536 336 us, with gelu 414; 8192^3 1095 us,
-//                 1004 TFLOP/s, two thirds of a library product's rate).
+//                 (214272 x 384 -> 1536, other operands in each call, 367 us, with gelu
+//                 431; 8192^3 1140 us, 965 TFLOP/s, 0.6 of a library product's rate).
 //
 // fp32: a step's values are split in registers into three bf16 planes of 8
-// bits each by cutting off (h + m + l is the value exactly), and six of the
-// nine products are formed; the others are at most 2^-23 of the whole.  Six bf16
+// bits each by cutting off (h + m + l is the value exactly, but for bits below
+// 2^-133), and six of the nine products are formed.  m is less than 2^-7 and l
+// less than 2^-15 of the value, so the others are at most 2^-21 of the product;
+// they have its sign, so what is missing leans towards zero.  Six bf16
 // instructions take 0.4 of the fp32 kind's time.  An infinity leaves NaN in its
 // lower planes: a NaN sum is formed again from the values.
 #include <hip/hip_runtime.h>

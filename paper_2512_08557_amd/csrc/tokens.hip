@@ -5,9 +5,9 @@
 // cosines and sines of their angles once for all heads in LDS, and then goes
 // through the tokens' heads, a head by G lanes with two 16-byte pieces each
 // (the same places of both halves of the head), whose sum of squares is
-// reduced between those lanes.  Every value is read and written once: 100000 fp32
-// tokens of 16 heads of 64 values 95 us, 5.1 TB/s, the rate of a copy; one token
-// 3.7 us, a launch, the positions' and the row's round trips.
+// reduced between those lanes.  Every value is read and written once: 60055 fp32
+// tokens of 8 query and 4 key heads of 64 values 95 us, 5.2 TB/s, the rate of a
+// copy; one token 3.6 us, a launch, the positions' and the row's round trips.
 //
 // The angle in turns is position * inv_freq / (2 pi) in 64 bits less its whole
 // part: a stream's stride number passes 10^6 within hours, where 32 bits would
@@ -279,8 +279,9 @@ int sscater_tokens_append(const sscater_head_spec* spec, const sscater_token_cac
     a.end0 = spec->section[0];
     a.end1 = spec->axes > 1 ? spec->section[0] + spec->section[1] : D / 2;
     a.eps = spec->eps;
-    // tokens of a workgroup: enough workgroups for the card, then longer ones (100000 fp32 tokens: one each 202 us, two
-    // 139, four 137, eight 140; 13000: 24.1, 20.1, 18.1, 18.8)
+    // tokens of a workgroup: enough workgroups for the card, then longer ones (8 query and 4 key heads of 64 values, one,
+    // two, four and eight tokens: 100000 bf16 tokens 204 us, 119, 80, 80; 100000 in fp32 209, 142, 146, 153; 13000 in fp32
+    // 23.5, 19.6, 17.9, 18.7)
     a.tt = std::min(APPEND_TOKENS, std::max(1, rows->tokens / 1024));
     const bool vec = (uintptr_t)qkv % 16 == 0 && a.ld * size % 16 == 0;
     if (size == 4) launch_append<true>(a, D, vec, (hipStream_t)stream);
