@@ -469,6 +469,109 @@ int sscater_tokens_attend(const sscater_attend_spec* spec, const sscater_token_c
 /* past[b] += the new tokens of sequence b. */
 int sscater_tokens_advance(const sscater_token_cache* cache, const sscater_token_rows* rows, void* stream);
 
+/* The norms before and after a block, with what lies between them, over rows:
+ *   t = act(gate) * P(block) * scale, sum = x + t, y = N(sum),
+ *   P(u) = (u - c) / sqrt(mean((u - c)^2) + eps) * block_weight + block_bias,
+ * c the mean of the row (center = 1) or zero; N the same with weight and bias.
+ * sum and y are formed from fp32 values and rounded once each (y from the sum
+ * before its rounding).
+ *   rows >= 0, width >= 1 (rows <= 2^36, width <= 2^30, rows * width <= 2^40);
+ *   block_norm = 0: block itself in P's place; activation (of the gate): NONE,
+ *   SILU or SIGMOID; gate_rows: consecutive rows that share a row of the gate
+ *   (1: a row for each; rows: one for all; rows must be a multiple);
+ *   *_stride: elements between two rows, at least width (of operands that are
+ *   there). */
+#define SSCATER_ACT_SIGMOID 4 /* 1 / (1 + exp(-z)), of gates */
+typedef struct {
+    int64_t rows, gate_rows;
+    int32_t width, dtype;  /* sscater_dtype */
+    int32_t center, block_norm, activation;
+    float eps;
+    int64_t x_stride, block_stride, gate_stride, sum_stride, y_stride;
+} sscater_norm_spec;
+
+/* x, block_weight, block_bias, gate, scale, weight, bias may be NULL (left out of
+ * the formulas; a null x is zero), and one of sum and y (not written; without y,
+ * weight and bias must be NULL too).  Rows [width] in dtype, aligned to their
+ * elements; weights, biases and scale [width].  sum or y may be x, block or a gate
+ * of as many rows (same pointer and stride); otherwise they overlap nothing. */
+int sscater_norm(const sscater_norm_spec* spec, const void* x, const void* block, const void* block_weight,
+                 const void* block_bias, const void* gate, const void* scale, const void* weight, const void* bias,
+                 void* sum, void* y, void* stream);
+
+/* Attention of one set of tokens to another, for `batch` sequences: queries (of
+ * objects, say) to keys and values (of a map's cells).  Sequence b's queries are
+ * rows q_start[b] to q_start[b + 1] - 1, its keys k_start[b] to k_start[b + 1] - 1
+ * (device int32[batch + 1], increasing from 0 to queries and keys), or, both NULL,
+ * max_q and max_k rows each (queries = batch * max_q, keys = batch * max_k).
+ *   q rows: q_heads heads of head_dim values; k and v rows: kv_heads heads;
+ *   *_stride: elements from row to row, at least a row's length, at most 2^24, of
+ *   k and v (pointers too) multiples of 16 bytes, as of q;
+ *   head_dim 32, 64 or 128; q_heads a multiple of kv_heads, at most 2^16;
+ *   queries, keys <= 2^30, batch <= 2^24, max_q * q_heads / kv_heads <= 2^30. */
+typedef struct {
+    int32_t dtype; /* sscater_dtype */
+    int32_t batch, q_heads, kv_heads, head_dim;
+    int32_t queries, keys, max_q, max_k;
+    float scale;
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t* q_start;
+    const int32_t* k_start;
+} sscater_cross_spec;
+
+/* out[i][h] = sum_j softmax_j(scale * q_i . k_j) v_j over the visible keys j of
+ * i's sequence, query head h reading key and value head h / (q_heads / kv_heads);
+ * zeros where no key is visible.  mask: device bytes [keys], zero where a key is
+ * not visible (its k and v are not read), or NULL; out: device [queries][q_heads]
+ * [head_dim], on a 16-byte boundary.  Queries behind the last sequence's are left
+ * as they were.  Precision as sscater_tokens_attend: scores, maxima and sums fp32;
+ * bf16 probabilities are rounded to bf16 for their product with the values where a
+ * sequence may bring more than 32 rows (max_q * q_heads / kv_heads).
+ * workspace: as there, sscater_cross_workspace() bytes (masked: also without
+ * splits).  `masked`: whether there will be a mask. */
+int sscater_cross_workspace(const sscater_cross_spec* spec, int32_t masked, size_t* bytes);
+int sscater_cross_attend(const sscater_cross_spec* spec, const void* q, const void* k, const void* v,
+                         const uint8_t* mask, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gated delta rule: a memory of fixed size for each of `batch` streams and
+ * `heads` value heads, state: device float [batch][heads][key_dim][value_dim] on a
+ * 16-byte boundary, which every token corrects and reads:
+ *   u = beta (v - alpha S^T k),  S <- alpha S + k u^T,  out = scale S^T q.
+ *   qk_heads divides heads: value head h takes query and key head
+ *   h / (heads / qk_heads); key_dim and value_dim 32, 64 or 128; batch <= 2^24,
+ *   heads <= 2^16. */
+typedef struct {
+    int32_t dtype; /* of the tokens, sscater_dtype */
+    int32_t batch, heads, qk_heads, key_dim, value_dim;
+    float* state;
+} sscater_delta_memory;
+
+/*   unit = 1: queries and keys are taken to unit length first, x / sqrt(sum x^2 +
+ *   eps); *_stride: elements from token to token. */
+typedef struct {
+    int32_t unit;
+    float eps, scale;
+    int64_t q_stride, k_stride, v_stride, a_stride, b_stride;
+} sscater_delta_spec;
+
+/* The new tokens of every stream, one after the other.  rows as above (max_past is
+ * not used): q, k [tokens][qk_heads][key_dim], v [tokens][heads][value_dim], a and b
+ * [tokens][heads], all in dtype, aligned to their elements; out [tokens][heads]
+ * [value_dim], on a 16-byte boundary.
+ *   rate, bias device float[heads]: alpha = exp(-rate softplus(a + bias)), beta =
+ *   1 / (1 + exp(-b)); both NULL: alpha = exp(a) (a <= 0, minus infinity forgets
+ *   everything), beta = b;
+ *   initial: states to begin from instead of memory->state, which is written all the
+ *   same (a copy of it where a stream has no tokens), or NULL.
+ * Everything is computed in fp32.  Rows behind the last stream's are left as they
+ * were.  The workspace is as for attention. */
+int sscater_delta_workspace(const sscater_delta_spec* spec, const sscater_delta_memory* memory,
+                            const sscater_token_rows* rows, size_t* bytes);
+int sscater_delta_update(const sscater_delta_spec* spec, const sscater_delta_memory* memory,
+                         const sscater_token_rows* rows, const float* initial, const void* q, const void* k,
+                         const void* v, const void* a, const void* b, const float* rate, const float* bias, void* out,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static text for an error code; for SSCATER_E_HIP the last HIP error text of
  * the calling thread's most recent failing call. */
 const char* sscater_strerror(int code);

@@ -1,0 +1,202 @@
+// Attention of one set of tokens to another: a call's mask turned into lists of
+// visible keys, and the attention kernel (attend_kernel.h) over the keys as they lie
+// or over the listed ones.
+//
+// Keys have no order, so the visible ones of a sequence may as well be the only
+// ones: their rows' numbers, one behind the other, are all that the attention looks
+// at, and cells that are not visible cost nothing but their byte of the mask.
+#include "attend_kernel.h"
+
+#include <algorithm>
+#include <cmath>
+#include <limits>
+
+namespace ssc {
+
+constexpr int LIST_KEYS = 16384;                       // of a workgroup: sixteen each of 1024 threads
+
+// Visible keys among sixteen of a mask from `at` on, of n: a bit for each byte that is not zero.
+__device__ __forceinline__ uint32_t seen16(const uint8_t* mask, int at, int n) {
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (at + 16 <= n) {
+        __builtin_memcpy(w, mask + at, 16);
+    } else {
+        for (int i = 0; at + i < n && i < 16; ++i) w[i >> 2] |= (uint32_t)mask[at + i] << (8 * (i & 3));
+    }
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = (((w[i] & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w[i]) & 0x80808080u;
+        bits |= ((x * 0x00204081u) >> 28 & 15u) << (4 * i);
+    }
+    return bits;
+}
+
+// A sequence's visible keys in order.  Workgroup b * parts + p lists those among the p-th
+// LIST_KEYS of sequence b, behind the ones before them, which it counts itself: a second
+// launch would take longer than reading a mask again.
+__global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRows keys, int32_t* list, int32_t* count,
+                                                    int parts, int64_t id0) {
+    __shared__ int sums[2][16];
+    const int64_t id = id0 + blockIdx.x;
+    const int b = (int)(id / parts), t = threadIdx.x;
+    int first, n;
+    rows_of(keys, b, first, n);
+    const int part = (int)(id % parts) * LIST_KEYS;
+    if (part >= n && part > 0) return;
+    mask += first;
+    int before = 0;
+    for (int at = t * 16; at < part; at += LIST_KEYS) before += __popc(seen16(mask, at, n));
+    uint32_t bits = part + t * 16 < n ? seen16(mask, part + t * 16, n) : 0;
+    int mine = __popc(bits), upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        before += __shfl_xor(before, o);
+        const int v = __shfl_up(upto, o);
+        if ((t & 63) >= o) upto += v;
+    }
+    if ((t & 63) == 63) {
+        sums[0][t >> 6] = before;
+        sums[1][t >> 6] = upto;
+    }
+    __syncthreads();
+    int base = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+        base += sums[0][w] + (w < (t >> 6) ? sums[1][w] : 0);
+        all += sums[0][w] + sums[1][w];
+    }
+    int32_t* to = list + first + base + upto - mine;
+    while (bits) {
+        *to++ = part + t * 16 + __ffs(bits) - 1;
+        bits &= bits - 1;
+    }
+    if (t == 0 && part + LIST_KEYS >= n) count[b] = all;
+}
+
+namespace {
+
+// What a call needs of its workspace: the splits' sums, the lists, their lengths.
+struct CrossPlan {
+    AttendCut cut;
+    size_t part, list, all;
+};
+
+bool cross_plan(const sscater_cross_spec* s, bool masked, CrossPlan* p) {
+    if (!s || (s->dtype != SSCATER_F32 && s->dtype != SSCATER_BF16)) return false;
+    if (s->batch < 1 || s->batch > (1 << 24) || s->kv_heads < 1 || s->q_heads < 1 || s->q_heads > (1 << 16) ||
+        s->q_heads % s->kv_heads || (s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128))
+        return false;
+    if (!(s->scale == s->scale) || (s->q_start == nullptr) != (s->k_start == nullptr) || (uintptr_t)s->q_start % 4 ||
+        (uintptr_t)s->k_start % 4)
+        return false;
+    auto rows_ok = [&](int64_t all, int64_t most) {
+        return all >= 0 && all <= (1 << 30) && most >= 0 && most <= all && (s->q_start || most * s->batch == all);
+    };
+    if (!rows_ok(s->queries, s->max_q) || !rows_ok(s->keys, s->max_k)) return false;
+    const int64_t size = s->dtype == SSCATER_F32 ? 4 : 2, q = (int64_t)s->q_heads * s->head_dim,
+                  kv = (int64_t)s->kv_heads * s->head_dim, most = 1 << 24;
+    if (s->q_stride < q || s->k_stride < kv || s->v_stride < kv || s->q_stride > most || s->k_stride > most ||
+        s->v_stride > most || s->q_stride * size % 16 || s->k_stride * size % 16 || s->v_stride * size % 16)
+        return false;
+    const int64_t rows = (int64_t)s->max_q * (s->q_heads / s->kv_heads);
+    if (rows > (1 << 30) || (int64_t)s->queries * s->q_heads > (int64_t(1) << 40)) return false;
+    cut_keys(&p->cut, s->dtype == SSCATER_F32, s->head_dim, rows, (int64_t)s->kv_heads * s->batch, s->max_k);
+    if (p->cut.grid > 0x7FFFFFFF) return false;
+    p->part = p->cut.splits > 1 ? (size_t)p->cut.splits * s->queries * s->q_heads * (s->head_dim + 2) * 4 : 0;
+    p->part = (p->part + 15) / 16 * 16;
+    p->list = p->part;
+    p->all = masked && s->keys > 0 ? p->list + ((size_t)s->keys + s->batch) * 4 : p->part;
+    return true;
+}
+
+template <bool F32, int D, Keys SRC>
+void launch_cross(AttendArgs a, const AttendCut& cut, hipStream_t s) {
+    const dim3 block(256);
+    for (int64_t at = 0; at < cut.grid; at += LAUNCH_GROUPS) {
+        a.id0 = (int)at;
+        const dim3 grid((unsigned)std::min(LAUNCH_GROUPS, cut.grid - at));
+        if constexpr (!(F32 && D == 128)) {
+            if (cut.wm == 1) attend_kernel<F32, D, 1, SRC><<<grid, block, 0, s>>>(a);
+        }
+        if (cut.wm == 2) attend_kernel<F32, D, 2, SRC><<<grid, block, 0, s>>>(a);
+        if (cut.wm == 4) attend_kernel<F32, D, 4, SRC><<<grid, block, 0, s>>>(a);
+    }
+    if (cut.splits > 1) {                              // at most some hundred thousand rows: see cut_keys
+        const int64_t rows = (int64_t)a.rows.tokens * a.q_heads;
+        join_kernel<F32, D, false><<<dim3((unsigned)((rows + 3) / 4)), block, 0, s>>>(a.part, a.out, rows, cut.splits,
+                                                                                      a.q_heads, rows_end(a.rows));
+    }
+}
+
+template <bool F32, Keys SRC>
+void launch_cross(const AttendArgs& a, const AttendCut& cut, int dim, hipStream_t s) {
+    if (dim == 32) launch_cross<F32, 32, SRC>(a, cut, s);
+    else if (dim == 64) launch_cross<F32, 64, SRC>(a, cut, s);
+    else launch_cross<F32, 128, SRC>(a, cut, s);
+}
+
+}  // namespace
+
+}  // namespace ssc
+
+using namespace ssc;
+
+extern "C" {
+
+int sscater_cross_workspace(const sscater_cross_spec* spec, int32_t masked, size_t* bytes) {
+    CrossPlan p;
+    if (!bytes || masked < 0 || masked > 1 || !cross_plan(spec, masked != 0, &p)) return SSCATER_E_INVALID_ARG;
+    *bytes = p.all;
+    return SSCATER_OK;
+}
+
+int sscater_cross_attend(const sscater_cross_spec* spec, const void* q, const void* k, const void* v,
+                         const uint8_t* mask, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    CrossPlan p;
+    if (!cross_plan(spec, mask != nullptr, &p)) return SSCATER_E_INVALID_ARG;
+    if (spec->queries == 0) return SSCATER_OK;
+    for (const void* x : {q, (const void*)out})
+        if (!x || (uintptr_t)x % 16) return SSCATER_E_INVALID_ARG;
+    for (const void* x : {k, v})
+        if ((!x && spec->keys > 0) || (uintptr_t)x % 16) return SSCATER_E_INVALID_ARG;
+    if (p.all > 0 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < p.all)) return SSCATER_E_INVALID_ARG;
+    const bool f32 = spec->dtype == SSCATER_F32, listed = mask != nullptr && spec->keys > 0;
+    const uint32_t size = f32 ? 4 : 2;
+    AttendArgs a{};
+    a.rows.tokens = spec->queries; a.rows.max_new = spec->max_q; a.rows.batch = spec->batch;
+    a.rows.start = spec->q_start; a.rows.past = nullptr;
+    a.q = q; a.k = k; a.v = v; a.out = out; a.part = (float*)workspace;
+    a.q_heads = spec->q_heads; a.kv_heads = spec->kv_heads; a.group = spec->q_heads / spec->kv_heads;
+    a.qtiles = p.cut.qtiles; a.splits = p.cut.splits;
+    // not zero, so that a masked score times it stays -inf; the least number of all, times a finite score, is zero beside 1
+    a.scale = std::max(std::fabs(spec->scale) * 1.4426950408889634f, std::numeric_limits<float>::denorm_min());
+    a.flip = spec->scale < 0.f ? f32 ? 0x80000000u : 0x80008000u : 0u;
+    a.pitch_q = spec->q_stride * size;
+    a.pitch_k = (uint32_t)spec->k_stride * size; a.pitch_v = (uint32_t)spec->v_stride * size;
+    a.keys = spec->keys; a.max_k = spec->max_k; a.k_start = spec->k_start;
+    if (listed) {
+        int32_t* list = (int32_t*)((char*)workspace + p.list);
+        a.list = list;
+        a.count = list + spec->keys;
+        TokenRows keys;
+        keys.tokens = spec->keys; keys.max_new = spec->max_k; keys.batch = spec->batch; keys.start = spec->k_start;
+        keys.past = nullptr;
+        const int64_t parts = std::max(1, (spec->max_k + LIST_KEYS - 1) / LIST_KEYS), groups = parts * spec->batch;
+        constexpr int64_t LAUNCH = LAUNCH_GROUPS / 4;  // workgroups of 1024 threads
+        for (int64_t id = 0; id < groups; id += LAUNCH)
+            list_kernel<<<dim3((unsigned)std::min(LAUNCH, groups - id)), dim3(1024), 0, (hipStream_t)stream>>>(
+                mask, keys, list, list + spec->keys, (int)parts, id);
+    }
+    if (f32) {
+        if (listed) launch_cross<true, Keys::LISTED>(a, p.cut, spec->head_dim, (hipStream_t)stream);
+        else launch_cross<true, Keys::ROWS>(a, p.cut, spec->head_dim, (hipStream_t)stream);
+    } else {
+        if (listed) launch_cross<false, Keys::LISTED>(a, p.cut, spec->head_dim, (hipStream_t)stream);
+        else launch_cross<false, Keys::ROWS>(a, p.cut, spec->head_dim, (hipStream_t)stream);
+    }
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SSCATER_OK : report_hip_error(e);
+}
+
+}  // extern "C"

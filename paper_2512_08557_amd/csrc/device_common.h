@@ -518,6 +518,12 @@ __device__ __forceinline__ void copy16(const void* src, lds_char* lds) {
                                      (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
+// 4 bytes per lane (lane l to lds + 4*l)
+__device__ __forceinline__ void copy4(const void* src, lds_char* lds) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                     (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
+}
+
 __device__ __forceinline__ uint4 lds16(const lds_char* p) {
     typedef uint32_t u4v __attribute__((ext_vector_type(4)));
     const u4v v = *reinterpret_cast<const __attribute__((address_space(3))) u4v*>(p);

@@ -28,7 +28,9 @@ EXPORTS = ("sscater_create", "sscater_create_neck", "sscater_create_pfn", "sscat
            "sscater_step_points",
            "sscater_read", "sscater_reset", "sscater_destroy", "sscater_changed", "sscater_changed_noalloc",
            "sscater_stats", "sscater_profile", "sscater_profile_read", "sscater_linear", "sscater_tokens_append",
-           "sscater_tokens_workspace", "sscater_tokens_attend", "sscater_tokens_advance", "sscater_strerror")
+           "sscater_tokens_workspace", "sscater_tokens_attend", "sscater_tokens_advance", "sscater_norm",
+           "sscater_cross_workspace", "sscater_cross_attend", "sscater_delta_workspace", "sscater_delta_update",
+           "sscater_strerror")
 
 
 class Grid(ctypes.Structure):
@@ -91,6 +93,34 @@ class AttendSpec(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+class NormSpec(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("gate_rows", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("center", ctypes.c_int32), ("block_norm", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("eps", ctypes.c_float), ("x_stride", ctypes.c_int64),
+                ("block_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64), ("sum_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64)]
+
+
+class CrossSpec(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("queries", ctypes.c_int32),
+                ("keys", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("q_start", ctypes.c_void_p), ("k_start", ctypes.c_void_p)]
+
+
+class DeltaMemorySpec(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("qk_heads", ctypes.c_int32), ("key_dim", ctypes.c_int32), ("value_dim", ctypes.c_int32),
+                ("state", ctypes.c_void_p)]
+
+
+class DeltaSpec(ctypes.Structure):
+    _fields_ = [("unit", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("a_stride", ctypes.c_int64), ("b_stride", ctypes.c_int64)]
+
+
 class SscaterError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -137,6 +167,12 @@ def lib() -> ctypes.CDLL:
         L.sscater_tokens_workspace.argtypes = [ctypes.POINTER(AttendSpec), cp, rp, ctypes.POINTER(ctypes.c_size_t)]
         L.sscater_tokens_attend.argtypes = [ctypes.POINTER(AttendSpec), cp, rp, vp, vp, vp, ctypes.c_size_t, vp]
         L.sscater_tokens_advance.argtypes = [cp, rp, vp]
+        xp, mp, dp = ctypes.POINTER(CrossSpec), ctypes.POINTER(DeltaMemorySpec), ctypes.POINTER(DeltaSpec)
+        L.sscater_norm.argtypes = [ctypes.POINTER(NormSpec)] + [vp] * 11
+        L.sscater_cross_workspace.argtypes = [xp, i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.sscater_cross_attend.argtypes = [xp] + [vp] * 6 + [ctypes.c_size_t, vp]
+        L.sscater_delta_workspace.argtypes = [dp, mp, rp, ctypes.POINTER(ctypes.c_size_t)]
+        L.sscater_delta_update.argtypes = [dp, mp, rp] + [vp] * 10 + [ctypes.c_size_t, vp]
         L.sscater_strerror.argtypes = [ctypes.c_int]
         L.sscater_strerror.restype = ctypes.c_char_p
         for f in EXPORTS[:-1]:
