@@ -8,9 +8,26 @@
 // rows of columns 4 c .. 4 c + 3, so a product with the state is key_dim / 2
 // multiplications a lane and a sum between eight neighbouring lanes, and q and k come
 // as one run of values for each lane.
+//
+// Stretches of 64 tokens at once: with G the running sum of log(alpha) within one, the
+// corrections u are the solution of a triangular system that no state is in,
+//
+//   (I + A) U = X,  A_ij = beta_i e^(G_i - G_j) k_i . k_j (j < i),  X = beta (V - e^G K S)
+//   O = scale (e^G Q S + P U),  P_ij = e^(G_i - G_j) q_i . k_j (j <= i)
+//   S <- e^G_63 S + (e^(G_63 - G) K)^T U
+//
+// so T = (I + A)^-1 and P are formed for all stretches at once (chunk_kernel), and what is
+// left from one to the next is five matrix products (state_kernel), each workgroup with 16
+// columns of a state.  They are products of fp32 values in the fp32 instructions: the state
+// that goes from stretch to stretch keeps its 24 bits.  A 16 x 16 result has its rows 4 g ..
+// 4 g + 3 in lane 16 g + column, which is also where the next product wants its second
+// operand's rows if the first's columns come in the same order, so S, X and U pass from
+// product to product as they stand, between wavefronts through LDS.  Exponents are
+// differences of sums in 64 bits: e^G_j may be zero where e^(G_i - G_j) is not.
 #include "tokens.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ssc {
 
@@ -150,7 +167,447 @@ __global__ __launch_bounds__(256) void delta_token_kernel(DeltaArgs a) {
     for (int i = 0; i < R; ++i) *(f4v*)(a.state + at + i * DV) = s[i];
 }
 
+// ---- stretches of tokens ----------------------------------------------------
+
+constexpr int CHUNK = 64;
+// What is kept of a stretch for each head: the ten lower tiles of T and of P, each as a wavefront reads it as a first
+// operand (lane 16 g + r: row r, columns 4 g .. 4 g + 3), four factors of every token, e^G_63 and whether something is
+// infinite or NaN.
+constexpr int MATS_P = 10 * 256, MATS_TOKEN = 20 * 256, MATS_LAST = MATS_TOKEN + 4 * CHUNK, MATS = MATS_LAST + 16;
+enum { TOKEN_K, TOKEN_U, TOKEN_Q, TOKEN_BETA };
+
+__device__ __forceinline__ int lower(int i, int j) { return i * (i + 1) / 2 + j; }
+
+__device__ __forceinline__ f4v mfma4(float x, float y, f4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, c, 0, 0, 0);
+}
+
+// A product of 16 x 16 tiles.
+__device__ __forceinline__ f4v tile_product(const f4v x, const f4v y, f4v c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = mfma4(x[e], y[e], c);
+    return c;
+}
+
+// The stretch that workgroup `slot` of a call has: a sequence's are first / CHUNK + b onwards, as many as it needs at most.
+__device__ __forceinline__ int slot_of(int first, int b) { return first / CHUNK + b; }
+
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
+
+template <bool F32, int DK>
+__global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
+    constexpr int NF = F32 ? DK / 16 : DK / 32;        // 16-byte pieces of a row that a lane holds
+    constexpr int TILE = 16 * 20;                      // 16 rows of 16 values, 20 apart: rows on different banks
+    __shared__ __attribute__((aligned(16))) float amat[10 * TILE], pmat[10 * TILE];
+    // keys as operands, then T
+    __shared__ __attribute__((aligned(16))) float shared[(4 * NF * 256 > 10 * TILE ? 4 * NF * 256 : 10 * TILE)];
+    __shared__ double total[CHUNK];
+    __shared__ float beta[CHUNK], unit_k[CHUNK], unit_q[CHUNK];
+    __shared__ int bad[4];
+    const int64_t id = a.item0 + blockIdx.x;
+    const int h = (int)(id % a.heads), slot = (int)(id / a.heads);
+    int lo = 0, hi = a.rows.batch - 1;
+    int first, n;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        rows_of(a.rows, mid, first, n);
+        if (slot_of(first, mid) <= slot) lo = mid; else hi = mid - 1;
+    }
+    rows_of(a.rows, lo, first, n);
+    const int c = slot - slot_of(first, lo);
+    if (c < 0 || c >= (n + CHUNK - 1) / CHUNK) return;
+    const int m = min(CHUNK, n - c * CHUNK);
+    const int64_t t0 = first + c * CHUNK;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int wq = 3 - w, hk = h / a.group;            // its row tile of Q: as many tiles of P as the others have of A
+    bool odd = false;
+    // rows 16 w + r of K and 16 wq + r of Q
+    uint4 kf[NF], qf[NF];
+    {
+        const int tk = 16 * w + r, tq = 16 * wq + r;
+        constexpr int E = F32 ? 4 : 8;
+        const char* pk = (const char*)a.k + ((t0 + min(tk, m - 1)) * a.ldk + hk * DK) * (F32 ? 4 : 2) + g * 16;
+        const char* pq = (const char*)a.q + ((t0 + min(tq, m - 1)) * a.ldq + hk * DK) * (F32 ? 4 : 2) + g * 16;
+        float kk = 0.f, qq = 0.f;
+#pragma unroll
+        for (int t = 0; t < NF; ++t) {
+            __builtin_memcpy(&kf[t], pk + t * 64, 16);
+            __builtin_memcpy(&qf[t], pq + t * 64, 16);
+            if (tk >= m) kf[t] = make_uint4(0, 0, 0, 0);
+            if (tq >= m) qf[t] = make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < NF; ++t) {
+            const uint32_t ku[4] = {kf[t].x, kf[t].y, kf[t].z, kf[t].w}, qu[4] = {qf[t].x, qf[t].y, qf[t].z, qf[t].w};
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float kv = __uint_as_float(F32 ? ku[e & 3] : e & 1 ? ku[e / 2] & 0xFFFF0000u : ku[e / 2] << 16);
+                const float qv = __uint_as_float(F32 ? qu[e & 3] : e & 1 ? qu[e / 2] & 0xFFFF0000u : qu[e / 2] << 16);
+                odd |= !finite(kv);
+                kk = fmaf(kv, kv, kk);
+                qq = fmaf(qv, qv, qq);
+            }
+            *(uint4*)&shared[((w * NF + t) * 64 + lane) * 4] = kf[t];
+        }
+        kk += __shfl_xor(kk, 16);
+        qq += __shfl_xor(qq, 16);
+        kk += __shfl_xor(kk, 32);
+        qq += __shfl_xor(qq, 32);
+        if (g == 0) {
+            unit_k[tk] = a.unit ? 1.f / sqrtf(kk + a.eps) : 1.f;
+            unit_q[tq] = (a.unit ? 1.f / sqrtf(qq + a.eps) : 1.f) * a.scale;
+        }
+    }
+    if (w == 0) {
+        const bool raw = a.rate != nullptr, live = lane < m;
+        const int64_t t = t0 + min(lane, m - 1);
+        const float la = log_alpha(value_at<F32>(a.a, t * a.lda + h), raw ? a.rate[h] : 0.f, raw ? a.bias[h] : 0.f, raw);
+        const float be = beta_of(value_at<F32>(a.b, t * a.ldb + h), raw);
+        odd |= live && !(finite(la) && finite(be));
+        double sum = live ? la : 0.;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const double v = __shfl_up(sum, o);
+            if (lane >= o) sum += v;
+        }
+        total[lane] = sum;
+        beta[lane] = live ? be : 0.f;
+    }
+    odd = __ballot(odd) != 0;
+    if (lane == 0) bad[w] = odd;
+    __syncthreads();
+    auto dot = [&](const uint4 (&x)[NF], int j) __attribute__((always_inline)) {
+        f4v c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < NF; ++t) {
+            const uint4 y = *(const uint4*)&shared[((j * NF + t) * 64 + lane) * 4];
+            if constexpr (F32) {
+                const uint32_t u[4] = {x[t].x, x[t].y, x[t].z, x[t].w}, v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c = mfma4(__uint_as_float(u[e]), __uint_as_float(v[e]), c);
+            } else {
+                c = mfma_bf16(x[t], y, c);
+            }
+        }
+        return c;
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const double gj = total[16 * j + r];
+        const float kj = unit_k[16 * j + r];
+        if (j <= w) {
+            const f4v d = dot(kf, j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 16 * w + 4 * g + e;
+                const float f = beta[i] * unit_k[i] * kj * expf((float)(total[i] - gj));
+                amat[lower(w, j) * TILE + (4 * g + e) * 20 + r] = 16 * j + r < i ? f * d[e] : 0.f;
+            }
+        }
+        if (j <= wq) {
+            const f4v d = dot(qf, j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = 16 * wq + 4 * g + e;
+                const float f = unit_q[i] * kj * expf((float)(total[i] - gj));
+                pmat[lower(wq, j) * TILE + (4 * g + e) * 20 + r] = 16 * j + r <= i ? f * d[e] : 0.f;
+            }
+        }
+    }
+    __syncthreads();
+    float* const out = mats + id * MATS;
+    // T's diagonal tile w by substitution, a column a lane (four times the same)
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        x[i] = i == r ? 1.f : 0.f;
+#pragma unroll
+        for (int k4 = 0; k4 < (i + 3) / 4; ++k4) {
+            const f4v v = *(const f4v*)&amat[lower(w, w) * TILE + i * 20 + 4 * k4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (4 * k4 + e < i) x[i] = fmaf(-v[e], x[4 * k4 + e], x[i]);
+        }
+    }
+    f4v column[4];                                     // T's tiles (i, w), i >= w
+    f4v diag;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) diag[e] = g == 0 ? x[e] : g == 1 ? x[4 + e] : g == 2 ? x[8 + e] : x[12 + e];
+    auto keep = [&](int i, const f4v v) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) shared[lower(i, w) * TILE + (4 * g + e) * 20 + r] = v[e];
+    };
+    auto operand = [&](const float* from, int tile) __attribute__((always_inline)) {
+        return *(const f4v*)&from[tile * TILE + r * 20 + 4 * g];
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i == w) {
+            column[i] = diag;
+            keep(i, diag);
+        }
+    __syncthreads();
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+        if (i > w) {
+            f4v y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < i; ++k)
+                if (k >= w) y = tile_product(operand(amat, lower(i, k)), column[k], y);
+            y = tile_product(operand(shared, lower(i, i)), y, f4v{0.f, 0.f, 0.f, 0.f});
+            column[i] = -y;
+            keep(i, column[i]);
+        }
+    __syncthreads();
+    for (int t = w; t < 10; t += 4) {
+        *(f4v*)&out[t * 256 + lane * 4] = operand(shared, t);
+        *(f4v*)&out[MATS_P + t * 256 + lane * 4] = operand(pmat, t);
+    }
+    if (w == 0) {
+        const float since = expf((float)total[lane]), left = expf((float)(total[CHUNK - 1] - total[lane]));
+        out[MATS_TOKEN + TOKEN_K * CHUNK + lane] = beta[lane] * since * unit_k[lane];
+        out[MATS_TOKEN + TOKEN_U * CHUNK + lane] = left * unit_k[lane];
+        out[MATS_TOKEN + TOKEN_Q * CHUNK + lane] = since * unit_q[lane];
+        out[MATS_TOKEN + TOKEN_BETA * CHUNK + lane] = beta[lane];
+        if (lane == CHUNK - 1) out[MATS_LAST] = since;
+        if (lane == 0) out[MATS_LAST + 1] = bad[0] | bad[1] | bad[2] | bad[3] ? 1.f : 0.f;
+    }
+}
+
+template <bool F32, int DK, int DV>
+__global__ __launch_bounds__(256) void state_kernel(DeltaArgs a, const float* mats) {
+    constexpr int NT = DK / 16, OWN = (NT + 3) / 4;    // row tiles of the state, and those of a wavefront
+    __shared__ __attribute__((aligned(16))) f4v sbuf[NT][64], zbuf[NT][64], xbuf[4][64], ubuf[4][64];
+    __shared__ float part[2][16][16];
+    __shared__ uint32_t bad[4];
+    // the columns of a head follow one another on one XCD (workgroup id mod 8), whose L2 then has its keys and matrices
+    const int64_t id = a.item0 + blockIdx.x, which = id / 8 / (DV / 16) * 8 + id % 8;
+    if (which >= (int64_t)a.rows.batch * a.heads) return;
+    const int b = (int)(which / a.heads), h = (int)(which % a.heads), hk = h / a.group;
+    int first, n;
+    rows_of(a.rows, b, first, n);
+    if (n == 0 && a.from == a.state) return;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int wq = 3 - w, col = (int)(id / 8 % (DV / 16)) * 16 + r;
+    const int chunks = (n + CHUNK - 1) / CHUNK;
+    const float* const mat = mats + ((int64_t)slot_of(first, b) * a.heads + h) * MATS;
+    f4v s[OWN];
+    auto state_at = [&](int o, int e) __attribute__((always_inline)) {
+        return (which * DK + 16 * (w + 4 * o) + 4 * g + e) * DV + col;
+    };
+#pragma unroll
+    for (int o = 0; o < OWN; ++o)
+        if (w + 4 * o < NT) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[o][e] = a.from[state_at(o, e)];
+            sbuf[w + 4 * o][lane] = s[o];
+        }
+    // what a stretch's products take from memory
+    struct Operands {
+        f4v k[NT], q[NT], kt[OWN][4], m[5], fk, fb, fq, fu[4];
+        float v[4], last, odd;
+    };
+    auto load = [&](int c, Operands& x) __attribute__((always_inline)) {
+        const int m = min(CHUNK, n - c * CHUNK);
+        const int64_t t0 = first + c * CHUNK;
+        const float* const mc = mat + (int64_t)c * a.heads * MATS;
+        auto row = [&](int t) __attribute__((always_inline)) { return t0 + min(t, m - 1); };
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float v[4];
+            values_at<F32>(a.k, row(16 * w + r) * a.ldk + hk * DK + 16 * t + 4 * g, v);
+            x.k[t] = f4v{v[0], v[1], v[2], v[3]};
+            values_at<F32>(a.q, row(16 * wq + r) * a.ldq + hk * DK + 16 * t + 4 * g, v);
+            x.q[t] = f4v{v[0], v[1], v[2], v[3]};
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = 16 * w + 4 * g + e;
+            x.v[e] = value_at<F32>(a.v, row(t) * a.ldv + h * DV + col);
+            if (t >= m) x.v[e] = 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int o = 0; o < OWN; ++o)
+                if (w + 4 * o < NT)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x.kt[o][t][e] = value_at<F32>(a.k, row(16 * t + 4 * g + e) * a.ldk + hk * DK + 16 * (w + 4 * o) + r);
+            x.fu[t] = *(const f4v*)&mc[MATS_TOKEN + TOKEN_U * CHUNK + 16 * t + 4 * g];
+        }
+        // tiles (w, 0 ..) of T, then (wq, 0 ..) of P: five in all
+#pragma unroll
+        for (int i = 0; i < 5; ++i)
+            x.m[i] = *(const f4v*)&mc[(i <= w ? lower(w, 0) + i : 10 + lower(wq, 0) + i - w - 1) * 256 + lane * 4];
+        x.fk = *(const f4v*)&mc[MATS_TOKEN + TOKEN_K * CHUNK + 16 * w + 4 * g];
+        x.fb = *(const f4v*)&mc[MATS_TOKEN + TOKEN_BETA * CHUNK + 16 * w + 4 * g];
+        x.fq = *(const f4v*)&mc[MATS_TOKEN + TOKEN_Q * CHUNK + 16 * wq + 4 * g];
+        x.last = mc[MATS_LAST];
+        x.odd = mc[MATS_LAST + 1];
+    };
+    auto put = [&](int64_t t, float v) __attribute__((always_inline)) {
+        const int64_t to = (t * a.heads + h) * DV + col;
+        if constexpr (F32) ((float*)a.out)[to] = v;
+        else ((uint16_t*)a.out)[to] = (uint16_t)bf16_pair(v, v);
+    };
+    // Tokens one by one, for columns with infinities or NaN in a stretch (all of them, if in its keys or gates): a product
+    // with a triangle's zeros would carry them to the tokens before.  Thread 16 p + column has the p-th sixteenth of a
+    // column's rows; the state after goes to zbuf.
+    auto slowly = [&](int c, uint32_t columns) __attribute__((always_inline)) {
+        constexpr int R = DK / 16;
+        const int p = threadIdx.x >> 4, m = min(CHUNK, n - c * CHUNK);
+        const bool raw = a.rate != nullptr;
+        const float rate = raw ? a.rate[h] : 0.f, bias = raw ? a.bias[h] : 0.f;
+        float z[R];
+        auto place = [&](f4v (&buf)[NT][64], int i) __attribute__((always_inline)) {
+            const int row = p * R + i;
+            return &((float*)&buf[row / 16][16 * (row % 16 / 4) + r])[row % 4];
+        };
+#pragma unroll
+        for (int i = 0; i < R; ++i) z[i] = *place(sbuf, i);
+        auto sum = [&](float v, int turn) __attribute__((always_inline)) {
+            part[turn][p][r] = v;
+            __syncthreads();
+            v = 0.f;
+            for (int i = 0; i < 16; ++i) v += part[turn][i][r];
+            return v;
+        };
+        for (int i = 0; i < m; ++i) {
+            const int64_t t = first + (int64_t)c * CHUNK + i;
+            float kk = 0.f, qq = 0.f, k[R], q[R];
+            values_at<F32>(a.k, t * a.ldk + hk * DK + p * R, k);
+            values_at<F32>(a.q, t * a.ldq + hk * DK + p * R, q);
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                kk = fmaf(k[j], k[j], kk);
+                qq = fmaf(q[j], q[j], qq);
+            }
+            const float fk = a.unit ? 1.f / sqrtf(sum(kk, 0) + a.eps) : 1.f;
+            const float fq = (a.unit ? 1.f / sqrtf(sum(qq, 1) + a.eps) : 1.f) * a.scale;
+            const float alpha = expf(log_alpha(value_at<F32>(a.a, t * a.lda + h), rate, bias, raw));
+            float dot = 0.f, o = 0.f;
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                k[j] *= fk;
+                dot = fmaf(z[j], k[j], dot);
+            }
+            const float u = beta_of(value_at<F32>(a.b, t * a.ldb + h), raw) *
+                            (value_at<F32>(a.v, t * a.ldv + h * DV + col) - alpha * sum(dot, 0));
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                z[j] = fmaf(k[j], u, alpha * z[j]);
+                o = fmaf(z[j], q[j], o);
+            }
+            o = sum(o, 1) * fq;
+            if (p == 0 && (columns >> r & 1)) put(t, o);
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) *place(zbuf, i) = z[i];
+    };
+    auto step = [&](int c, const Operands& x) __attribute__((always_inline)) {
+        const int m = min(CHUNK, n - c * CHUNK);
+        f4v z[NT], xs = {0.f, 0.f, 0.f, 0.f}, o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < NT; ++t) z[t] = sbuf[t][lane];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) xs = tile_product(x.k[t], z[t], xs);
+        bool odd = x.odd != 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            xs[e] = fmaf(x.fb[e], x.v[e], -x.fk[e] * xs[e]);
+            odd |= !finite(x.v[e]);
+        }
+        xbuf[w][lane] = xs;
+        const uint64_t lanes = __ballot(odd);
+        if (lane == 0) bad[w] = (uint32_t)(lanes | lanes >> 32) | (uint32_t)(lanes >> 16 | lanes >> 48);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o = tile_product(x.q[t], z[t], o);
+        lds_barrier();
+        const uint32_t columns = __builtin_amdgcn_readfirstlane((bad[0] | bad[1] | bad[2] | bad[3]) & 0xFFFFu);
+        if (columns) slowly(c, columns);
+        f4v u = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (t <= w) u = tile_product(x.m[t], xbuf[t][lane], u);
+        ubuf[w][lane] = u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= x.fq[e];
+#pragma unroll
+        for (int i = 0; i < OWN; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[i][e] *= x.last;
+        lds_barrier();
+        f4v us[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) us[t] = ubuf[t][lane];
+#pragma unroll
+        for (int i = 0; i < OWN; ++i)
+            if (w + 4 * i < NT) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    f4v y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = us[t][e] * x.fu[t][e];
+                    s[i] = tile_product(x.kt[i][t], y, s[i]);
+                }
+                if (columns >> r & 1) s[i] = zbuf[w + 4 * i][lane];
+                sbuf[w + 4 * i][lane] = s[i];
+            }
+#pragma unroll
+        for (int i = 1; i < 5; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (i == w + 1 + t) o = tile_product(x.m[i], us[t], o);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = 16 * wq + 4 * g + e;
+            if (t < m && !(columns >> r & 1)) put(first + (int64_t)c * CHUNK + t, o[e]);
+        }
+        lds_barrier();
+    };
+    Operands x, y;
+    if (chunks > 0) load(0, x);
+    lds_barrier();
+    for (int c = 0; c < chunks; c += 2) {
+        if (c + 1 < chunks) load(c + 1, y);
+        step(c, x);
+        if (c + 1 >= chunks) break;
+        if (c + 2 < chunks) load(c + 2, x);
+        step(c + 1, y);
+    }
+#pragma unroll
+    for (int o = 0; o < OWN; ++o)
+        if (w + 4 * o < NT)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a.state[state_at(o, e)] = s[o][e];
+}
+
 namespace {
+
+// Whether a call's tokens are taken in stretches.
+bool in_chunks(const sscater_token_rows* r) { return r->max_new >= 32; }
+
+int64_t chunk_slots(const sscater_delta_memory* m, const sscater_token_rows* r) {
+    return (int64_t)r->tokens / CHUNK + m->batch;
+}
+
+template <bool F32, int DK>
+void launch_chunks(DeltaArgs a, int64_t slots, float* mats, hipStream_t s) {
+    for (int64_t g = 0; g < slots * a.heads; g += LAUNCH_GROUPS) {
+        a.item0 = g;
+        chunk_kernel<F32, DK><<<dim3((unsigned)std::min(LAUNCH_GROUPS, slots * a.heads - g)), dim3(256), 0, s>>>(a, mats);
+    }
+}
+
+template <bool F32, int DK, int DV>
+void launch_states(DeltaArgs a, const float* mats, hipStream_t s) {
+    const int64_t groups = ((int64_t)a.rows.batch * a.heads + 7) / 8 * 8 * (DV / 16);
+    for (int64_t g = 0; g < groups; g += LAUNCH_GROUPS) {
+        a.item0 = g;
+        state_kernel<F32, DK, DV><<<dim3((unsigned)std::min(LAUNCH_GROUPS, groups - g)), dim3(256), 0, s>>>(a, mats);
+    }
+}
 
 template <bool F32, int DK, int DV>
 void launch_tokens(DeltaArgs a, hipStream_t s) {
@@ -162,17 +619,24 @@ void launch_tokens(DeltaArgs a, hipStream_t s) {
 }
 
 template <bool F32, int DK>
-void launch_delta(const DeltaArgs& a, int dv, hipStream_t s) {
+void launch_delta(const DeltaArgs& a, int dv, int64_t slots, float* mats, hipStream_t s) {
+    if (mats) {
+        launch_chunks<F32, DK>(a, slots, mats, s);
+        if (dv == 32) launch_states<F32, DK, 32>(a, mats, s);
+        else if (dv == 64) launch_states<F32, DK, 64>(a, mats, s);
+        else launch_states<F32, DK, 128>(a, mats, s);
+        return;
+    }
     if (dv == 32) launch_tokens<F32, DK, 32>(a, s);
     else if (dv == 64) launch_tokens<F32, DK, 64>(a, s);
     else launch_tokens<F32, DK, 128>(a, s);
 }
 
 template <bool F32>
-void launch_delta(const DeltaArgs& a, int dk, int dv, hipStream_t s) {
-    if (dk == 32) launch_delta<F32, 32>(a, dv, s);
-    else if (dk == 64) launch_delta<F32, 64>(a, dv, s);
-    else launch_delta<F32, 128>(a, dv, s);
+void launch_delta(const DeltaArgs& a, int dk, int dv, int64_t slots, float* mats, hipStream_t s) {
+    if (dk == 32) launch_delta<F32, 32>(a, dv, slots, mats, s);
+    else if (dk == 64) launch_delta<F32, 64>(a, dv, slots, mats, s);
+    else launch_delta<F32, 128>(a, dv, slots, mats, s);
 }
 
 bool head_size(int d) { return d == 32 || d == 64 || d == 128; }
@@ -203,7 +667,7 @@ extern "C" {
 int sscater_delta_workspace(const sscater_delta_spec* spec, const sscater_delta_memory* memory,
                             const sscater_token_rows* rows, size_t* bytes) {
     if (!bytes || !delta_ok(spec, memory, rows)) return SSCATER_E_INVALID_ARG;
-    *bytes = 0;
+    *bytes = in_chunks(rows) ? (size_t)chunk_slots(memory, rows) * memory->heads * MATS * 4 : 0;
     return SSCATER_OK;
 }
 
@@ -221,6 +685,9 @@ int sscater_delta_update(const sscater_delta_spec* spec, const sscater_delta_mem
     } else if (!initial || initial == memory->state) {
         return SSCATER_OK;
     }
+    size_t need = 0;
+    sscater_delta_workspace(spec, memory, rows, &need);
+    if (need > 0 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return SSCATER_E_INVALID_ARG;
     DeltaArgs x;
     x.rows.tokens = rows->tokens; x.rows.max_new = rows->max_new; x.rows.batch = memory->batch;
     x.rows.start = rows->tokens ? rows->start : nullptr; x.rows.past = nullptr;
@@ -230,8 +697,10 @@ int sscater_delta_update(const sscater_delta_spec* spec, const sscater_delta_mem
     x.ldq = spec->q_stride; x.ldk = spec->k_stride; x.ldv = spec->v_stride; x.lda = spec->a_stride; x.ldb = spec->b_stride;
     x.heads = memory->heads; x.group = memory->heads / memory->qk_heads;
     x.unit = spec->unit; x.eps = spec->eps; x.scale = spec->scale; x.item0 = 0;
-    if (size == 4) launch_delta<true>(x, memory->key_dim, memory->value_dim, (hipStream_t)stream);
-    else launch_delta<false>(x, memory->key_dim, memory->value_dim, (hipStream_t)stream);
+    float* const mats = in_chunks(rows) ? (float*)workspace : nullptr;
+    const int64_t slots = chunk_slots(memory, rows);
+    if (size == 4) launch_delta<true>(x, memory->key_dim, memory->value_dim, slots, mats, (hipStream_t)stream);
+    else launch_delta<false>(x, memory->key_dim, memory->value_dim, slots, mats, (hipStream_t)stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SSCATER_OK : report_hip_error(e);
 }

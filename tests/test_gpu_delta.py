@@ -225,6 +225,39 @@ def test_streams_do_not_meet(n):
     assert torch.equal(c.memory.state[same], state[same])
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("where", ["q", "k", "v", "a", "b"])
+@pytest.mark.parametrize("at,value", [(70, math.nan), (85, math.inf), (0, -math.inf), (129, math.nan)])
+def test_no_token_sees_a_later_one(at, value, where, kind):
+    """An infinity or NaN in a token reaches none of those before it (nor, in a query,
+    those after), and no stream beside it."""
+    c = Case(15, [150, 90], 2, 1, 64, 32, kind)
+    rows = [(i, s, S, err, ref, tol) for i, s, S, err, ref, tol in c.sequences()]
+    t = getattr(c, where)
+    if where == "v":
+        t[at, 1, 3] = value
+    elif where in "ab":
+        t[at, 1] = value
+    else:
+        t[at, 0, 5] = value
+    out = c.call(start=c.start, max_new=150)
+    (_, s0, _, _, ref, tol), (_, s1, S, err, ref1, tol1) = rows
+    bound(out[s0][:at], ref[:at], tol[:at], f"before {where}")
+    bound(out[s1], ref1, tol1, "the other stream")
+    assert bool(((c.memory.state[1].double().cpu() - S).norm(dim=1) <= err + 2 * U * S.norm(dim=1)).all())
+    if where == "q":
+        bound(out[s0][at + 1:], ref[at + 1:], tol[at + 1:], "after a query")
+    elif where == "v":
+        assert not bool(torch.isfinite(out[s0][at:, 1, 3]).any())
+        out[:, 1, 3] = torch.where(torch.isfinite(out[:, 1, 3]), out[:, 1, 3], ref[0, 0, 0].to(out))
+        keep = [i for i in range(32) if i != 3]
+        bound(out[s0][:, 1, keep], ref[:, 1, keep], tol[:, 1, keep], "the other values")
+    if where in "vab":
+        bound(out[s0][:, 0], ref[:, 0], tol[:, 0], "the other head")
+    if where == "k":
+        assert not bool(torch.isfinite(out[s0][at:]).any())
+
+
 @pytest.mark.parametrize("n", [1, 130])
 def test_a_captured_update_replays(n):
     rng = np.random.default_rng(12)
