@@ -47,6 +47,7 @@ struct DeltaArgs {
     int64_t item0;         // first wavefront of the launch
     int heads, group;      // value heads, and those that share a query and key head
     int unit;
+    int parts, length;     // of a stream, and the stretches of one
     float eps, scale;
 };
 
@@ -68,6 +69,26 @@ __device__ __forceinline__ void values_at(const void* p, int64_t i, float (&v)[N
         for (int e = 0; e < N; ++e) v[e] = __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
     }
 }
+
+// Values as they lie in memory, made fp32 where they are used: a conversion beside the load would wait for it there.
+template <bool F32>
+struct Raw4 {
+    uint32_t w[F32 ? 4 : 2];
+    __device__ __forceinline__ void load(const void* p, int64_t i) {
+        __builtin_memcpy(w, (const char*)p + i * (F32 ? 4 : 2), sizeof w);
+    }
+    __device__ __forceinline__ f4v get() const {
+        if constexpr (F32) return f4v{__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3])};
+        else return f4v{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u), __uint_as_float(w[1] << 16),
+                        __uint_as_float(w[1] & 0xFFFF0000u)};
+    }
+};
+template <bool F32>
+struct Raw1 {
+    typename std::conditional<F32, uint32_t, uint16_t>::type w;
+    __device__ __forceinline__ void load(const void* p, int64_t i) { w = ((const decltype(w)*)p)[i]; }
+    __device__ __forceinline__ float get() const { return __uint_as_float(F32 ? (uint32_t)w : (uint32_t)w << 16); }
+};
 
 // The sum over eight neighbouring lanes, the same bits in all of them.
 __device__ __forceinline__ float sum8(float v) {
@@ -374,89 +395,197 @@ __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
     }
 }
 
-template <bool F32, int DK, int DV>
-__global__ __launch_bounds__(256) void state_kernel(DeltaArgs a, const float* mats) {
+// From one stretch to the next.  A workgroup has 16 columns of a head's state; wavefronts 0 to 3 take it through the
+// stretches (X, then U, then S), 4 to 7 form the outputs beside them, so that a SIMD's two wavefronts fill each other's
+// waits.  An operand of the next stretch is loaded into its registers as soon as this one's product has taken them; every
+// load is made whatever the stretch, so that the number under way is known where they are waited for.
+//
+// Where streams and heads leave compute units idle, a stream is cut into a.parts of a.length stretches.  A part takes S
+// to M S + B, so a first launch (OUT = false) takes zeros (the first part: the state, and puts it aside too) and, in more
+// columns, the unit matrix through all parts but the last, without outputs, and the workgroups of the second begin with
+// the product of the parts before theirs.
+template <bool F32, int DK, int DV, bool OUT>
+__global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, const float* mats, float* parts) {
+    constexpr int S = F32 ? 4 : 2;
     constexpr int NT = DK / 16, OWN = (NT + 3) / 4;    // row tiles of the state, and those of a wavefront
     __shared__ __attribute__((aligned(16))) f4v sbuf[NT][64], zbuf[NT][64], xbuf[4][64], ubuf[4][64];
     __shared__ float part[2][16][16];
     __shared__ uint32_t bad[4];
     // the columns of a head follow one another on one XCD (workgroup id mod 8), whose L2 then has its keys and matrices
-    const int64_t id = a.item0 + blockIdx.x, which = id / 8 / (DV / 16) * 8 + id % 8;
+    constexpr int BLOCKS = (OUT ? DV : DV + DK) / 16;
+    const int64_t id = a.item0 + blockIdx.x, of = id / 8 / BLOCKS;
+    const int64_t which = of / (OUT ? a.parts : a.parts - 1) * 8 + id % 8;
+    const int seg = (int)(of % (OUT ? a.parts : a.parts - 1)), block = (int)(id / 8 % BLOCKS);
     if (which >= (int64_t)a.rows.batch * a.heads) return;
     const int b = (int)(which / a.heads), h = (int)(which % a.heads), hk = h / a.group;
     int first, n;
     rows_of(a.rows, b, first, n);
-    if (n == 0 && a.from == a.state) return;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int wq = 3 - w, col = (int)(id / 8 % (DV / 16)) * 16 + r;
-    const int chunks = (n + CHUNK - 1) / CHUNK;
+    const bool unit = !OUT && block >= DV / 16;        // columns of the unit matrix
+    const int all = (n + CHUNK - 1) / CHUNK, c0 = min(all, seg * a.length), chunks = min(all, c0 + a.length);
+    if (OUT && n == 0 && a.from == a.state) return;
+    if (seg > 0 ? c0 == all : unit) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int w = wave & 3, wq = 3 - w, col = (block - (unit ? DV / 16 : 0)) * 16 + r;
+    // a part's M, as first operands, and B, as results
+    constexpr int PART = DK * DK + DK * DV;
+    float* const part0 = parts + which * a.parts * PART;
+    auto b_of = [&](int j, int tile) __attribute__((always_inline)) {
+        return (f4v*)(part0 + j * PART + DK * DK + ((int64_t)tile * (DV / 16) + block) * 256 + lane * 4);
+    };
     const float* const mat = mats + ((int64_t)slot_of(first, b) * a.heads + h) * MATS;
+    const uint32_t ldk = (uint32_t)a.ldk * S, ldq = (uint32_t)a.ldq * S, ldv = (uint32_t)a.ldv * S;
+    auto tokens = [&](int c) __attribute__((always_inline)) { return min(CHUNK, n - c * CHUNK); };
+    auto put = [&](int64_t t, float v) __attribute__((always_inline)) {
+        const int64_t to = (t * a.heads + h) * DV + col;
+        if constexpr (F32) ((float*)a.out)[to] = v;
+        else ((uint16_t*)a.out)[to] = (uint16_t)bf16_pair(v, v);
+    };
+    // the same from all of a workgroup's wavefronts
+    auto bad_columns = [&]() __attribute__((always_inline)) {
+        return __builtin_amdgcn_readfirstlane((bad[0] | bad[1] | bad[2] | bad[3]) & 0xFFFFu);
+    };
+    const int sums = a.unit ? 4 : 2;                   // of a token taken by itself
+
+    if (OUT && wave >= 4) {
+        Raw4<F32> q[NT];
+        f4v p[4], fq;
+        uint32_t off = (uint32_t)(16 * wq + r) * ldq + 4 * g * S;
+        auto load_q = [&](int c) __attribute__((always_inline)) {
+            const int64_t t0 = first + (int64_t)c * CHUNK;
+            const char* const at = (const char*)a.q + (t0 * a.ldq + hk * DK) * S;
+            const int m = tokens(c);
+            if (m < CHUNK) off = (uint32_t)min(16 * wq + r, m - 1) * ldq + 4 * g * S;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) q[t].load(at + off + 16 * t * S, 0);
+            fq = *(const f4v*)&mat[(int64_t)c * a.heads * MATS + MATS_TOKEN + TOKEN_Q * CHUNK + 16 * wq + 4 * g];
+        };
+        auto load_p = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                p[i] = *(const f4v*)&mat[(int64_t)c * a.heads * MATS + MATS_P + lower(wq, min(i, wq)) * 256 + lane * 4];
+        };
+        if (chunks > c0) {
+            load_q(c0);
+            load_p(c0);
+        }
+        lds_barrier();
+        for (int j = 1; j < seg; ++j) {
+            lds_barrier();
+            lds_barrier();
+        }
+#pragma unroll 1
+        for (int c = c0; c < chunks; ++c) {
+            const int m = tokens(c), next = min(c + 1, chunks - 1);
+            lds_barrier();
+            const uint32_t columns = bad_columns();
+            if (columns)
+                for (int i = m * sums; i > 0; --i) lds_barrier();
+            f4v o[2] = {};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) o[t & 1] = tile_product(q[t].get(), sbuf[t][lane], o[t & 1]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                o[0][e] = (o[0][e] + o[1][e]) * fq[e];
+                o[1][e] = 0.f;
+            }
+            load_q(next);
+            lds_barrier();
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (t <= wq) o[t & 1] = tile_product(p[t], ubuf[t][lane], o[t & 1]);
+            load_p(next);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int t = 16 * wq + 4 * g + e;
+                if (t < m && !(columns >> r & 1)) put(first + (int64_t)c * CHUNK + t, o[0][e] + o[1][e]);
+            }
+            lds_barrier();
+        }
+        return;
+    }
+
     f4v s[OWN];
+    auto tile = [&](int o) __attribute__((always_inline)) { return NT < 4 ? min(w, NT - 1) : w + 4 * o; };
+    const bool own = NT >= 4 || w < NT;
     auto state_at = [&](int o, int e) __attribute__((always_inline)) {
-        return (which * DK + 16 * (w + 4 * o) + 4 * g + e) * DV + col;
+        return (which * DK + 16 * tile(o) + 4 * g + e) * DV + col;
     };
 #pragma unroll
-    for (int o = 0; o < OWN; ++o)
-        if (w + 4 * o < NT) {
+    for (int o = 0; o < OWN; ++o) {
+        if (OUT && a.parts > 1) {
+            // the state put aside, or the first part's end
+            s[o] = *b_of(seg == 0 ? a.parts - 1 : 0, tile(o));
+        } else if (seg == 0) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[o][e] = a.from[state_at(o, e)];
-            sbuf[w + 4 * o][lane] = s[o];
+            if (!OUT && own) *b_of(a.parts - 1, tile(o)) = s[o];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[o][e] = unit && 16 * tile(o) + 4 * g + e == col ? 1.f : 0.f;
         }
-    // what a stretch's products take from memory
-    struct Operands {
-        f4v k[NT], q[NT], kt[OWN][4], m[5], fk, fb, fq, fu[4];
-        float v[4], last, odd;
+        if (own) sbuf[tile(o)][lane] = s[o];
+    }
+    Raw4<F32> k[NT];
+    Raw1<F32> kt[OWN][4][4], v[4];
+    f4v inv[4], fk, fb, fu[4];
+    float last, keys_odd;
+    uint32_t off_k = (uint32_t)(16 * w + r) * ldk + 4 * g * S, off_t[4][4], off_v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        off_v[e] = (uint32_t)(16 * w + 4 * g + e) * ldv + col * S;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) off_t[t][e] = (uint32_t)(16 * t + 4 * g + e) * ldk + (16 * tile(0) + r) * S;
+    }
+    auto keys_of = [&](int c) __attribute__((always_inline)) {
+        return (const char*)a.k + ((first + (int64_t)c * CHUNK) * a.ldk + hk * DK) * S;
     };
-    auto load = [&](int c, Operands& x) __attribute__((always_inline)) {
-        const int m = min(CHUNK, n - c * CHUNK);
-        const int64_t t0 = first + c * CHUNK;
+    // (the rows behind a stream's last token are that token once more)
+    auto load_x = [&](int c) __attribute__((always_inline)) {
+        const char* const at = (const char*)a.v + ((first + (int64_t)c * CHUNK) * a.ldv + h * DV) * S;
         const float* const mc = mat + (int64_t)c * a.heads * MATS;
-        auto row = [&](int t) __attribute__((always_inline)) { return t0 + min(t, m - 1); };
+        const int m = tokens(c);
+        if (m < CHUNK) {
+            off_k = (uint32_t)min(16 * w + r, m - 1) * ldk + 4 * g * S;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float v[4];
-            values_at<F32>(a.k, row(16 * w + r) * a.ldk + hk * DK + 16 * t + 4 * g, v);
-            x.k[t] = f4v{v[0], v[1], v[2], v[3]};
-            values_at<F32>(a.q, row(16 * wq + r) * a.ldq + hk * DK + 16 * t + 4 * g, v);
-            x.q[t] = f4v{v[0], v[1], v[2], v[3]};
+            for (int e = 0; e < 4; ++e) off_v[e] = (uint32_t)min(16 * w + 4 * g + e, m - 1) * ldv + col * S;
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int t = 16 * w + 4 * g + e;
-            x.v[e] = value_at<F32>(a.v, row(t) * a.ldv + h * DV + col);
-            if (t >= m) x.v[e] = 0.f;
+        for (int t = 0; t < NT; ++t) k[t].load(keys_of(c) + off_k + 16 * t * S, 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e].load(at + off_v[e], 0);
+        fk = *(const f4v*)&mc[MATS_TOKEN + TOKEN_K * CHUNK + 16 * w + 4 * g];
+        fb = *(const f4v*)&mc[MATS_TOKEN + TOKEN_BETA * CHUNK + 16 * w + 4 * g];
+        keys_odd = mc[MATS_LAST + 1];
+    };
+    auto load_u = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) inv[i] = *(const f4v*)&mat[(int64_t)c * a.heads * MATS + lower(w, min(i, w)) * 256 + lane * 4];
+    };
+    auto load_s = [&](int c) __attribute__((always_inline)) {
+        const float* const mc = mat + (int64_t)c * a.heads * MATS;
+        const int m = tokens(c);
+        if (m < CHUNK) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) off_t[t][e] = (uint32_t)min(16 * t + 4 * g + e, m - 1) * ldk + (16 * tile(0) + r) * S;
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int o = 0; o < OWN; ++o)
-                if (w + 4 * o < NT)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        x.kt[o][t][e] = value_at<F32>(a.k, row(16 * t + 4 * g + e) * a.ldk + hk * DK + 16 * (w + 4 * o) + r);
-            x.fu[t] = *(const f4v*)&mc[MATS_TOKEN + TOKEN_U * CHUNK + 16 * t + 4 * g];
+                for (int e = 0; e < 4; ++e) kt[o][t][e].load(keys_of(c) + off_t[t][e] + 64 * o * S, 0);
+            fu[t] = *(const f4v*)&mc[MATS_TOKEN + TOKEN_U * CHUNK + 16 * t + 4 * g];
         }
-        // tiles (w, 0 ..) of T, then (wq, 0 ..) of P: five in all
-#pragma unroll
-        for (int i = 0; i < 5; ++i)
-            x.m[i] = *(const f4v*)&mc[(i <= w ? lower(w, 0) + i : 10 + lower(wq, 0) + i - w - 1) * 256 + lane * 4];
-        x.fk = *(const f4v*)&mc[MATS_TOKEN + TOKEN_K * CHUNK + 16 * w + 4 * g];
-        x.fb = *(const f4v*)&mc[MATS_TOKEN + TOKEN_BETA * CHUNK + 16 * w + 4 * g];
-        x.fq = *(const f4v*)&mc[MATS_TOKEN + TOKEN_Q * CHUNK + 16 * wq + 4 * g];
-        x.last = mc[MATS_LAST];
-        x.odd = mc[MATS_LAST + 1];
-    };
-    auto put = [&](int64_t t, float v) __attribute__((always_inline)) {
-        const int64_t to = (t * a.heads + h) * DV + col;
-        if constexpr (F32) ((float*)a.out)[to] = v;
-        else ((uint16_t*)a.out)[to] = (uint16_t)bf16_pair(v, v);
+        last = mc[MATS_LAST];
     };
     // Tokens one by one, for columns with infinities or NaN in a stretch (all of them, if in its keys or gates): a product
     // with a triangle's zeros would carry them to the tokens before.  Thread 16 p + column has the p-th sixteenth of a
     // column's rows; the state after goes to zbuf.
     auto slowly = [&](int c, uint32_t columns) __attribute__((always_inline)) {
         constexpr int R = DK / 16;
-        const int p = threadIdx.x >> 4, m = min(CHUNK, n - c * CHUNK);
+        const int p = threadIdx.x >> 4, m = tokens(c);
         const bool raw = a.rate != nullptr;
         const float rate = raw ? a.rate[h] : 0.f, bias = raw ? a.bias[h] : 0.f;
         float z[R];
@@ -468,7 +597,7 @@ __global__ __launch_bounds__(256) void state_kernel(DeltaArgs a, const float* ma
         for (int i = 0; i < R; ++i) z[i] = *place(sbuf, i);
         auto sum = [&](float v, int turn) __attribute__((always_inline)) {
             part[turn][p][r] = v;
-            __syncthreads();
+            lds_barrier();                             // as many as the other wavefronts wait for: `sums` a token
             v = 0.f;
             for (int i = 0; i < 16; ++i) v += part[turn][i][r];
             return v;
@@ -493,94 +622,114 @@ __global__ __launch_bounds__(256) void state_kernel(DeltaArgs a, const float* ma
                 dot = fmaf(z[j], k[j], dot);
             }
             const float u = beta_of(value_at<F32>(a.b, t * a.ldb + h), raw) *
-                            (value_at<F32>(a.v, t * a.ldv + h * DV + col) - alpha * sum(dot, 0));
+                            ((unit ? 0.f : value_at<F32>(a.v, t * a.ldv + h * DV + col)) - alpha * sum(dot, 0));
 #pragma unroll
             for (int j = 0; j < R; ++j) {
                 z[j] = fmaf(k[j], u, alpha * z[j]);
                 o = fmaf(z[j], q[j], o);
             }
             o = sum(o, 1) * fq;
-            if (p == 0 && (columns >> r & 1)) put(t, o);
+            if (OUT && p == 0 && (columns >> r & 1)) put(t, o);
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) *place(zbuf, i) = z[i];
     };
-    auto step = [&](int c, const Operands& x) __attribute__((always_inline)) {
-        const int m = min(CHUNK, n - c * CHUNK);
-        f4v z[NT], xs = {0.f, 0.f, 0.f, 0.f}, o = {0.f, 0.f, 0.f, 0.f};
+    if (chunks > c0) {
+        load_x(c0);
+        load_u(c0);
+        load_s(c0);
+    }
+    lds_barrier();
+    if constexpr (OUT) {
+#pragma unroll 1
+        for (int j = 1; j < seg; ++j) {
+            f4v y[OWN];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) z[t] = sbuf[t][lane];
+            for (int o = 0; o < OWN; ++o) {
+                y[o] = *b_of(j, tile(o));
 #pragma unroll
-        for (int t = 0; t < NT; ++t) xs = tile_product(x.k[t], z[t], xs);
-        bool odd = x.odd != 0.f;
+                for (int t = 0; t < NT; ++t)
+                    y[o] = tile_product(*(const f4v*)(part0 + j * PART + (tile(o) * NT + t) * 256 + lane * 4), sbuf[t][lane], y[o]);
+            }
+            lds_barrier();
+#pragma unroll
+            for (int o = 0; o < OWN; ++o) {
+                s[o] = y[o];
+                if (own) sbuf[tile(o)][lane] = s[o];
+            }
+            lds_barrier();
+        }
+    }
+#pragma unroll 1
+    for (int c = c0; c < chunks; ++c) {
+        const int m = tokens(c), next = min(c + 1, chunks - 1);
+        // two sums: an instruction need not wait for the one before it
+        f4v x[2] = {};
+#pragma unroll
+        for (int t = 0; t < NT; ++t) x[t & 1] = tile_product(k[t].get(), sbuf[t][lane], x[t & 1]);
+        bool odd = keys_odd != 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            xs[e] = fmaf(x.fb[e], x.v[e], -x.fk[e] * xs[e]);
-            odd |= !finite(x.v[e]);
+            const float value = 16 * w + 4 * g + e < m && !unit ? v[e].get() : 0.f;
+            x[0][e] = fmaf(fb[e], value, -fk[e] * (x[0][e] + x[1][e]));
+            odd |= !finite(value);
         }
-        xbuf[w][lane] = xs;
+        xbuf[w][lane] = x[0];
         const uint64_t lanes = __ballot(odd);
         if (lane == 0) bad[w] = (uint32_t)(lanes | lanes >> 32) | (uint32_t)(lanes >> 16 | lanes >> 48);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) o = tile_product(x.q[t], z[t], o);
+        load_x(next);
         lds_barrier();
-        const uint32_t columns = __builtin_amdgcn_readfirstlane((bad[0] | bad[1] | bad[2] | bad[3]) & 0xFFFFu);
+        const uint32_t columns = bad_columns();
         if (columns) slowly(c, columns);
-        f4v u = {0.f, 0.f, 0.f, 0.f};
+        f4v u[2] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-            if (t <= w) u = tile_product(x.m[t], xbuf[t][lane], u);
-        ubuf[w][lane] = u;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] *= x.fq[e];
+            if (t <= w) u[t & 1] = tile_product(inv[t], xbuf[t][lane], u[t & 1]);
+        ubuf[w][lane] = u[0] + u[1];
 #pragma unroll
         for (int i = 0; i < OWN; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[i][e] *= x.last;
+            for (int e = 0; e < 4; ++e) s[i][e] *= last;
+        load_u(next);
         lds_barrier();
-        f4v us[4];
+        f4v more[OWN] = {};
 #pragma unroll
-        for (int t = 0; t < 4; ++t) us[t] = ubuf[t][lane];
+        for (int t = 0; t < 4; ++t) {
+            f4v y = ubuf[t][lane];
 #pragma unroll
-        for (int i = 0; i < OWN; ++i)
-            if (w + 4 * i < NT) {
+            for (int e = 0; e < 4; ++e) y[e] *= fu[t][e];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    f4v y;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = us[t][e] * x.fu[t][e];
-                    s[i] = tile_product(x.kt[i][t], y, s[i]);
-                }
-                if (columns >> r & 1) s[i] = zbuf[w + 4 * i][lane];
-                sbuf[w + 4 * i][lane] = s[i];
+            for (int i = 0; i < OWN; ++i) {
+                const f4v key = {kt[i][t][0].get(), kt[i][t][1].get(), kt[i][t][2].get(), kt[i][t][3].get()};
+                if (t & 1) more[i] = tile_product(key, y, more[i]);
+                else s[i] = tile_product(key, y, s[i]);
             }
-#pragma unroll
-        for (int i = 1; i < 5; ++i)
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (i == w + 1 + t) o = tile_product(x.m[i], us[t], o);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int t = 16 * wq + 4 * g + e;
-            if (t < m && !(columns >> r & 1)) put(first + (int64_t)c * CHUNK + t, o[e]);
         }
-        lds_barrier();
-    };
-    Operands x, y;
-    if (chunks > 0) load(0, x);
-    lds_barrier();
-    for (int c = 0; c < chunks; c += 2) {
-        if (c + 1 < chunks) load(c + 1, y);
-        step(c, x);
-        if (c + 1 >= chunks) break;
-        if (c + 2 < chunks) load(c + 2, x);
-        step(c + 1, y);
-    }
 #pragma unroll
-    for (int o = 0; o < OWN; ++o)
-        if (w + 4 * o < NT)
+        for (int i = 0; i < OWN; ++i) {
+            s[i] += more[i];
+            if (columns >> r & 1) s[i] = zbuf[tile(i)][lane];
+            if (own) sbuf[tile(i)][lane] = s[i];
+        }
+        load_s(next);
+        lds_barrier();
+    }
+    if (!own) return;
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) {
+        if (OUT) {
+            if (chunks < all) break;                   // a later part has the stream's end
 #pragma unroll
             for (int e = 0; e < 4; ++e) a.state[state_at(o, e)] = s[o][e];
+        } else if (!unit) {
+            *b_of(seg, tile(o)) = s[o];
+        } else {
+            // column 4 x + y of a tile is lane 16 x + row's y-th value of the operand
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                part0[seg * PART + (tile(o) * NT + col / 16) * 256 + ((r / 4) * 16 + 4 * g + e) * 4 + r % 4] = s[o][e];
+        }
+    }
 }
 
 namespace {
@@ -588,9 +737,13 @@ namespace {
 // Whether a call's tokens are taken in stretches.
 bool in_chunks(const sscater_token_rows* r) { return r->max_new >= 32; }
 
-int64_t chunk_slots(const sscater_delta_memory* m, const sscater_token_rows* r) {
-    return (int64_t)r->tokens / CHUNK + m->batch;
-}
+constexpr int MAX_PARTS = 64;
+
+// Stretches of a call, parts of a stream and the stretches of a part; no stretches: tokens one by one.
+struct DeltaPlan {
+    int64_t slots;
+    int parts, length;
+};
 
 template <bool F32, int DK>
 void launch_chunks(DeltaArgs a, int64_t slots, float* mats, hipStream_t s) {
@@ -600,13 +753,49 @@ void launch_chunks(DeltaArgs a, int64_t slots, float* mats, hipStream_t s) {
     }
 }
 
-template <bool F32, int DK, int DV>
-void launch_states(DeltaArgs a, const float* mats, hipStream_t s) {
-    const int64_t groups = ((int64_t)a.rows.batch * a.heads + 7) / 8 * 8 * (DV / 16);
-    for (int64_t g = 0; g < groups; g += LAUNCH_GROUPS) {
-        a.item0 = g;
-        state_kernel<F32, DK, DV><<<dim3((unsigned)std::min(LAUNCH_GROUPS, groups - g)), dim3(256), 0, s>>>(a, mats);
+// Parts of the streams: what makes both launches' rounds over the card shortest.  In microseconds, measured at heads of
+// 64 x 64: a stretch with its outputs 2.5 and without 1.6, a product of parts 0.8, a launch and its first loads 5.
+DeltaPlan delta_plan(const sscater_delta_memory* m, const sscater_token_rows* r) {
+    DeltaPlan p = {0, 1, 0};
+    if (!in_chunks(r)) return p;
+    p.slots = (int64_t)r->tokens / CHUNK + m->batch;
+    const int64_t heads = (int64_t)m->batch * m->heads, most = (r->max_new + CHUNK - 1) / CHUNK;
+    double best = 0.;
+    for (int64_t n = 1; n <= std::min(most, (int64_t)MAX_PARTS); ++n) {
+        const int64_t length = (most + n - 1) / n, out = heads * (m->value_dim / 16) * n,
+                      in = heads * ((m->value_dim + m->key_dim) / 16) * (n - 1);
+        if ((most + length - 1) / length != n || (n > 1 && out > 2048)) continue;
+        const double cost = length * (2.5 * ((out + 255) / 256) + (n > 1 ? 1.6 * ((in + 511) / 512) : 0.)) +
+                            (n > 1 ? 5. + 0.8 * (n - 2) : 0.);
+        if (n == 1 || cost < best) {
+            best = cost;
+            p.parts = (int)n;
+            p.length = (int)length;
+        }
     }
+    return p;
+}
+
+size_t delta_bytes(const DeltaPlan& p, const sscater_delta_memory* m) {
+    const size_t part = (size_t)m->key_dim * (m->key_dim + m->value_dim);
+    return 4 * m->heads * (p.slots * (size_t)MATS + (p.parts > 1 ? (size_t)m->batch * p.parts * part : 0));
+}
+
+template <bool F32, int DK, int DV, bool OUT>
+void launch_states(DeltaArgs a, const float* mats, float* parts, hipStream_t s) {
+    const int64_t groups = ((int64_t)a.rows.batch * a.heads + 7) / 8 * 8 * (OUT ? a.parts * (DV / 16) : (a.parts - 1) * ((DV + DK) / 16));
+    constexpr int THREADS = OUT ? 512 : 256;
+    constexpr int64_t LAUNCH = LAUNCH_GROUPS * 256 / THREADS;
+    for (int64_t g = 0; g < groups; g += LAUNCH) {
+        a.item0 = g;
+        state_kernel<F32, DK, DV, OUT><<<dim3((unsigned)std::min(LAUNCH, groups - g)), dim3(THREADS), 0, s>>>(a, mats, parts);
+    }
+}
+
+template <bool F32, int DK, int DV>
+void launch_states(const DeltaArgs& a, const float* mats, float* parts, hipStream_t s) {
+    if (a.parts > 1) launch_states<F32, DK, DV, false>(a, mats, parts, s);
+    launch_states<F32, DK, DV, true>(a, mats, parts, s);
 }
 
 template <bool F32, int DK, int DV>
@@ -620,11 +809,12 @@ void launch_tokens(DeltaArgs a, hipStream_t s) {
 
 template <bool F32, int DK>
 void launch_delta(const DeltaArgs& a, int dv, int64_t slots, float* mats, hipStream_t s) {
-    if (mats) {
+    if (slots) {
         launch_chunks<F32, DK>(a, slots, mats, s);
-        if (dv == 32) launch_states<F32, DK, 32>(a, mats, s);
-        else if (dv == 64) launch_states<F32, DK, 64>(a, mats, s);
-        else launch_states<F32, DK, 128>(a, mats, s);
+        float* const parts = mats + slots * a.heads * MATS;
+        if (dv == 32) launch_states<F32, DK, 32>(a, mats, parts, s);
+        else if (dv == 64) launch_states<F32, DK, 64>(a, mats, parts, s);
+        else launch_states<F32, DK, 128>(a, mats, parts, s);
         return;
     }
     if (dv == 32) launch_tokens<F32, DK, 32>(a, s);
@@ -653,7 +843,8 @@ bool delta_ok(const sscater_delta_spec* s, const sscater_delta_memory* m, const 
         return false;
     const int64_t qk = (int64_t)m->qk_heads * m->key_dim, v = (int64_t)m->heads * m->value_dim;
     return s->unit >= 0 && s->unit <= 1 && s->eps >= 0.f && s->scale == s->scale && s->q_stride >= qk &&
-           s->k_stride >= qk && s->v_stride >= v && s->a_stride >= m->heads && s->b_stride >= m->heads;
+           s->k_stride >= qk && s->v_stride >= v && s->a_stride >= m->heads && s->b_stride >= m->heads &&
+           std::max(s->q_stride, std::max(s->k_stride, s->v_stride)) <= (1 << 24);
 }
 
 }  // namespace
@@ -667,7 +858,7 @@ extern "C" {
 int sscater_delta_workspace(const sscater_delta_spec* spec, const sscater_delta_memory* memory,
                             const sscater_token_rows* rows, size_t* bytes) {
     if (!bytes || !delta_ok(spec, memory, rows)) return SSCATER_E_INVALID_ARG;
-    *bytes = in_chunks(rows) ? (size_t)chunk_slots(memory, rows) * memory->heads * MATS * 4 : 0;
+    *bytes = delta_bytes(delta_plan(memory, rows), memory);
     return SSCATER_OK;
 }
 
@@ -685,8 +876,8 @@ int sscater_delta_update(const sscater_delta_spec* spec, const sscater_delta_mem
     } else if (!initial || initial == memory->state) {
         return SSCATER_OK;
     }
-    size_t need = 0;
-    sscater_delta_workspace(spec, memory, rows, &need);
+    const DeltaPlan plan = delta_plan(memory, rows);
+    const size_t need = delta_bytes(plan, memory);
     if (need > 0 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return SSCATER_E_INVALID_ARG;
     DeltaArgs x;
     x.rows.tokens = rows->tokens; x.rows.max_new = rows->max_new; x.rows.batch = memory->batch;
@@ -697,10 +888,10 @@ int sscater_delta_update(const sscater_delta_spec* spec, const sscater_delta_mem
     x.ldq = spec->q_stride; x.ldk = spec->k_stride; x.ldv = spec->v_stride; x.lda = spec->a_stride; x.ldb = spec->b_stride;
     x.heads = memory->heads; x.group = memory->heads / memory->qk_heads;
     x.unit = spec->unit; x.eps = spec->eps; x.scale = spec->scale; x.item0 = 0;
-    float* const mats = in_chunks(rows) ? (float*)workspace : nullptr;
-    const int64_t slots = chunk_slots(memory, rows);
-    if (size == 4) launch_delta<true>(x, memory->key_dim, memory->value_dim, slots, mats, (hipStream_t)stream);
-    else launch_delta<false>(x, memory->key_dim, memory->value_dim, slots, mats, (hipStream_t)stream);
+    x.parts = plan.parts; x.length = plan.length;
+    float* const mats = (float*)workspace;
+    if (size == 4) launch_delta<true>(x, memory->key_dim, memory->value_dim, plan.slots, mats, (hipStream_t)stream);
+    else launch_delta<false>(x, memory->key_dim, memory->value_dim, plan.slots, mats, (hipStream_t)stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SSCATER_OK : report_hip_error(e);
 }

@@ -161,11 +161,13 @@ def test_gates(n, raw, unit, hard, kind):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
-def test_a_long_stream(kind):
-    """Thousands of tokens, one of the heads forgetting hardly anything."""
-    c = Case(3, [3000, 1500], 2, 2, 32, 32, kind)
+@pytest.mark.parametrize("counts,dk,dv", [([3000, 1500], 32, 32), ([1, 1000, 0, 640], 128, 32), ([2049], 64, 128)])
+def test_a_long_stream(counts, dk, dv, kind):
+    """Thousands of tokens, one of the heads forgetting hardly anything: streams in
+    parts, of which short ones have no second."""
+    c = Case(3, counts, 2, 2, dk, dv, kind)
     c.rate[0], c.bias[0] = 0.01, -7.0
-    c.check(start=c.start, max_new=3000)
+    c.check(start=c.start, max_new=max(counts))
 
 
 def test_parts_of_a_stream_are_the_stream():
@@ -187,10 +189,10 @@ def test_parts_of_a_stream_are_the_stream():
     assert bool(((c.memory.state[0].double().cpu() - S).norm(dim=1) <= err + 2 * U * S.norm(dim=1)).all())
 
 
-@pytest.mark.parametrize("n", [1, 100])
+@pytest.mark.parametrize("n", [1, 100, 1500])
 def test_initial_states(n):
     """Beginning from other states leaves those as they were and writes the memory's,
-    of streams without tokens too."""
+    of streams without tokens too; from its own gives the same bits."""
     c = Case(n, [n, 0, n], 2, 1, 32, 64, "f32")
     want = c.call(start=c.start, max_new=n).clone()
     state = c.memory.state.clone()
@@ -227,11 +229,12 @@ def test_streams_do_not_meet(n):
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("where", ["q", "k", "v", "a", "b"])
-@pytest.mark.parametrize("at,value", [(70, math.nan), (85, math.inf), (0, -math.inf), (129, math.nan)])
+@pytest.mark.parametrize("at,value", [(70, math.nan), (85, math.inf), (0, -math.inf), (129, math.nan), (700, math.inf)])
 def test_no_token_sees_a_later_one(at, value, where, kind):
     """An infinity or NaN in a token reaches none of those before it (nor, in a query,
-    those after), and no stream beside it."""
-    c = Case(15, [150, 90], 2, 1, 64, 32, kind)
+    those after), and no stream beside it; also where a stream is taken in parts."""
+    n = 150 if at < 150 else 1500
+    c = Case(15, [n, 90], 2, 1, 64, 32, kind)
     rows = [(i, s, S, err, ref, tol) for i, s, S, err, ref, tol in c.sequences()]
     t = getattr(c, where)
     if where == "v":
@@ -240,7 +243,7 @@ def test_no_token_sees_a_later_one(at, value, where, kind):
         t[at, 1] = value
     else:
         t[at, 0, 5] = value
-    out = c.call(start=c.start, max_new=150)
+    out = c.call(start=c.start, max_new=n)
     (_, s0, _, _, ref, tol), (_, s1, S, err, ref1, tol1) = rows
     bound(out[s0][:at], ref[:at], tol[:at], f"before {where}")
     bound(out[s1], ref1, tol1, "the other stream")
