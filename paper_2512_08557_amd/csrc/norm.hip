@@ -7,10 +7,13 @@
 // Every value is read and written once: a row's values stay in the registers of
 // the lanes that share it, in fp32, through both norms (a mean first and the
 // squares about it afterwards, of values that are there already), and y is formed
-// from the sum before that is rounded.
+// from the sum before that is rounded.  Those lanes take several rows, the next
+// one's values under way while this one's are worked on; what the rows share
+// (weights, an image's gate times the scale) stays in registers too.
 #include "tokens.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ssc {
 
@@ -29,28 +32,49 @@ struct NormArgs {
     int64_t ldx, ldb, ldg, lds, ldy;
     int64_t gate_rows;     // rows that share one of the gate's
     int width, lanes;      // lanes of a row
+    int each;              // rows of the same lanes
+    int whole;             // all their pieces are there
     int center, act, post;
     float eps;
 };
 
-// Values k.. of a row: sixteen bytes of them as fp32, zeros from `width` on.  Rows
-// may be aligned to their values only.
-template <bool F32, int E>
-__device__ __forceinline__ void load_piece(const void* row, int k, int width, float (&v)[E]) {
+// Sixteen bytes of a row, values k .. of it, and zeros from `width` on.  Rows may be aligned to their values only.
+template <bool F32>
+__device__ __forceinline__ uint4 load_raw(const void* row, int k, int width) {
+    constexpr int E = F32 ? 4 : 8;
     uint32_t u[4] = {0, 0, 0, 0};
     if (k + E <= width) {
         __builtin_memcpy(u, (const char*)row + (int64_t)k * (F32 ? 4 : 2), 16);
-    } else {
+    } else if (k < width) {
+        // the row's end: eight bytes, four, two, as many as there are
+        const int n = (width - k) * (F32 ? 4 : 2);
+        const char* at = (const char*)row + (int64_t)k * (F32 ? 4 : 2);
+        uint32_t w = 0;
+        if (n & 8) __builtin_memcpy(u, at, 8);
+        if (n & 4) __builtin_memcpy(&w, at + (n & 8), 4);
+        if ((n & 12) == 12) u[2] = w;
+        else if (n & 4) u[0] = w;
+        if constexpr (!F32) {
+            uint16_t h = 0;
+            if (n & 2) __builtin_memcpy(&h, at + (n & 12), 2);
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (k + e < width) {
-                if constexpr (F32) u[e] = ((const uint32_t*)row)[k + e];
-                else u[e / 2] |= (uint32_t)((const uint16_t*)row)[k + e] << (16 * (e & 1));
-            }
+            for (int i = 0; i < 4; ++i) u[i] = (n & 2) && n / 4 == i ? h : u[i];
+        }
     }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+template <bool F32, int E>
+__device__ __forceinline__ void unpack(const uint4 raw, float (&v)[E]) {
+    const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
     for (int e = 0; e < E; ++e)
         v[e] = F32 ? __uint_as_float(u[e]) : __uint_as_float(e & 1 ? u[e / 2] & 0xFFFF0000u : u[e / 2] << 16);
+}
+
+template <bool F32, int E>
+__device__ __forceinline__ void load_piece(const void* row, int k, int width, float (&v)[E]) {
+    unpack<F32>(load_raw<F32>(row, k, width), v);
 }
 
 template <bool F32, int E>
@@ -61,27 +85,45 @@ __device__ __forceinline__ void store_piece(void* row, int k, int width, const f
         if constexpr (F32) u[i] = __float_as_uint(v[i]);
         else u[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
     }
+    char* const at = (char*)row + (int64_t)k * (F32 ? 4 : 2);
     if (k + E <= width) {
-        __builtin_memcpy((char*)row + (int64_t)k * (F32 ? 4 : 2), u, 16);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (k + e < width) {
-                if constexpr (F32) ((uint32_t*)row)[k + e] = u[e];
-                else ((uint16_t*)row)[k + e] = (uint16_t)(u[e / 2] >> (16 * (e & 1)));
+        __builtin_memcpy(at, u, 16);
+    } else if (k < width) {
+        const int n = (width - k) * (F32 ? 4 : 2);
+        if (n & 8) __builtin_memcpy(at, u, 8);
+        if (n & 4) {
+            const uint32_t w = n & 8 ? u[2] : u[0];
+            __builtin_memcpy(at + (n & 8), &w, 4);
+        }
+        if constexpr (!F32)
+            if (n & 2) {
+                const uint16_t h = (uint16_t)(n & 8 ? n & 4 ? u[3] : u[2] : n & 4 ? u[1] : u[0]);
+                __builtin_memcpy(at + (n & 12), &h, 2);
             }
     }
 }
 
+// The exponential is of the product with log2(e) and, to first order, of that product's rounding: at -80 the rounding
+// alone would be 4e-6 of the result.
 __device__ __forceinline__ float gate_value(float g, int act) {
     if (act == SSCATER_ACT_NONE) return g;
-    const float s = 1.f / (1.f + expf(-g));
+    const float t = -1.44269504f * g, low = fmaf(-1.44269504f, g, -t) - 1.92596303e-8f * g, x = __builtin_amdgcn_exp2f(t);
+    const float s = __builtin_amdgcn_rcpf(1.f + (fabsf(t) < 126.f ? fmaf(x, 0.69314718f * low, x) : x));
     return act == SSCATER_ACT_SILU ? g * s : s;
 }
 
-// A row's sum over its lanes, at most a wavefront of them or the whole workgroup.
+// A row's sum over its lanes, at most a wavefront of them or the whole workgroup; the same bits in all.
 __device__ __forceinline__ float row_sum(float v, int lanes, float (&part)[2][4], int& turn) {
-    for (int o = 1; o < min(lanes, 64); o <<= 1) v += __shfl_xor(v, o);
+    auto add = [&](auto ctrl) __attribute__((always_inline)) {
+        constexpr int C = decltype(ctrl)::value;
+        v += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), C, 0xF, 0xF, true));
+    };
+    if (lanes > 1) add(std::integral_constant<int, 0xB1>{});       // the neighbour
+    if (lanes > 2) add(std::integral_constant<int, 0x4E>{});       // the other pair of four
+    if (lanes > 4) add(std::integral_constant<int, 0x141>{});      // the other four of eight, back to front
+    if (lanes > 8) add(std::integral_constant<int, 0x140>{});      // the other eight of sixteen, the same
+    if (lanes > 16) v += __shfl_xor(v, 16);
+    if (lanes > 32) v += __shfl_xor(v, 32);
     if (lanes > 64) {                                  // uniform: the launch's
         // two sets in turn: the next sum's writers need not wait for this one's readers
         if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = v;
@@ -93,30 +135,72 @@ __device__ __forceinline__ float row_sum(float v, int lanes, float (&part)[2][4]
 }
 
 // NP pieces of 16 bytes a lane; piece i of lane s of a row is its piece i * lanes + s.
+// Registers for two wavefronts a SIMD (NP = 1: four); the compiler left alone takes 261 for three pieces of bf16, and one
+// wavefront a SIMD is 254 us over four maps for 150.
 template <bool F32, int NP>
-__global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(256, (NP == 1 ? 4 : 2)) void norm_kernel(NormArgs a) {
     constexpr int S = F32 ? 4 : 2, E = 16 / S;
     __shared__ float part[2][4];
     int turn = 0;
     const int per = 256 / a.lanes, sub = threadIdx.x % a.lanes;
-    const int64_t at = a.row0 + (int64_t)blockIdx.x * per + threadIdx.x / a.lanes;
-    const int64_t row = min(at, a.rows - 1);           // lanes behind the last row take part in the sums
+    const int64_t first = a.row0 + ((int64_t)blockIdx.x * per + threadIdx.x / a.lanes) * a.each;
     auto piece = [&](int i) __attribute__((always_inline)) { return (i * a.lanes + sub) * E; };
-    float z[NP][E], x[NP][E], g[NP][E];
-    const char* block = (const char*)a.block + row * a.ldb * S;
+    uint4 w[NP], b[NP], bw[NP], bb[NP];
+    float gs[NP][E];                                   // act(gate) * scale
+    auto vector = [&](const void* v, uint4 (&to)[NP]) __attribute__((always_inline)) {
+        if (v)
 #pragma unroll
-    for (int i = 0; i < NP; ++i) load_piece<F32>(block, piece(i), a.width, z[i]);
-    if (a.x) {
+            for (int i = 0; i < NP; ++i) to[i] = load_raw<F32>(v, piece(i), a.width);
+    };
+    vector(a.w, w);
+    vector(a.b, b);
+    vector(a.bw, bw);
+    vector(a.bb, bb);
+    struct Row {
+        uint4 x[NP], z[NP];
+    };
+    // lanes behind the last row take part in the sums
+    auto load = [&](int64_t at, Row& r) __attribute__((always_inline)) {
+        const int64_t row = min(at, a.rows - 1);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) load_piece<F32>((const char*)a.x + row * a.ldx * S, piece(i), a.width, x[i]);
-    }
+        for (int i = 0; i < NP; ++i) r.z[i] = load_raw<F32>((const char*)a.block + row * a.ldb * S, piece(i), a.width);
+        if (a.x) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) r.x[i] = load_raw<F32>((const char*)a.x + row * a.ldx * S, piece(i), a.width);
+        }
+    };
+    auto factors = [&](int64_t row) __attribute__((always_inline)) {
+        uint4 g[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) g[i] = load_raw<F32>((const char*)a.gate + row * a.ldg * S, piece(i), a.width);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            unpack<F32>(g[i], gs[i]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) gs[i][e] = gate_value(gs[i][e], a.act);
+            if (a.scale) {
+                float v[E];
+                load_piece<F32>(a.scale, piece(i), a.width, v);
+#pragma unroll
+                for (int e = 0; e < E; ++e) gs[i][e] *= v[e];
+            }
+        }
+    };
+    // rows left of the gate's row, and that row
+    int64_t shared = 0, left = a.rows;
     if (a.gate) {
-        const char* gate = (const char*)a.gate + (a.gate_rows == 1 ? row : row / a.gate_rows) * a.ldg * S;
+        if (a.gate_rows > 1) {
+            const int64_t row = min(first, a.rows - 1);
+            shared = row >> 32 || a.gate_rows >> 32 ? row / a.gate_rows : (uint32_t)row / (uint32_t)a.gate_rows;
+            left = (shared + 1) * a.gate_rows - row;
+        }
+    } else if (a.scale) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) load_piece<F32>(gate, piece(i), a.width, g[i]);
+        for (int i = 0; i < NP; ++i) load_piece<F32>(a.scale, piece(i), a.width, gs[i]);
     }
     const float inv = 1.f / a.width;
-    auto normed = [&](const void* w, const void* b) __attribute__((always_inline)) {
+    float z[NP][E];
+    auto normed = [&](const void* wp, const uint4 (&wv)[NP], const void* bp, const uint4 (&bv)[NP]) __attribute__((always_inline)) {
         if (a.center) {
             float s = 0.f;
 #pragma unroll
@@ -127,7 +211,13 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
 #pragma unroll
             for (int i = 0; i < NP; ++i)
 #pragma unroll
-                for (int e = 0; e < E; ++e) z[i][e] = piece(i) + e < a.width ? z[i][e] - mean : 0.f;
+                for (int e = 0; e < E; ++e) z[i][e] -= mean;
+            if (!a.whole) {
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) z[i][e] = piece(i) + e < a.width ? z[i][e] : 0.f;
+            }
         }
         float s = 0.f;
 #pragma unroll
@@ -138,53 +228,67 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             float v[E], c[E];
-            if (w) load_piece<F32>(w, piece(i), a.width, v);
-            if (b) load_piece<F32>(b, piece(i), a.width, c);
+            if (wp) unpack<F32>(wv[i], v);
+            if (bp) unpack<F32>(bv[i], c);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 z[i][e] *= r;
-                if (w) z[i][e] *= v[e];
-                if (b) z[i][e] += c[e];
+                if (wp) z[i][e] *= v[e];
+                if (bp) z[i][e] += c[e];
             }
         }
     };
-    if (a.post) normed(a.bw, a.bb);
-    if (a.gate) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-#pragma unroll
-            for (int e = 0; e < E; ++e) z[i][e] *= gate_value(g[i][e], a.act);
-    }
-    if (a.scale) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            float v[E];
-            load_piece<F32>(a.scale, piece(i), a.width, v);
-#pragma unroll
-            for (int e = 0; e < E; ++e) z[i][e] *= v[e];
+    Row next;
+    load(first, next);
+    for (int i0 = 0; i0 < a.each; ++i0) {
+        const int64_t at = first + i0;
+        const Row r = next;
+        if (i0 + 1 < a.each) load(at + 1, next);
+        if (a.gate) {
+            if (a.gate_rows == 1) {
+                factors(min(at, a.rows - 1));
+            } else if (i0 == 0 || left == 0) {
+                if (i0 > 0 && at < a.rows) ++shared;
+                if (i0 > 0) left = a.gate_rows;
+                factors(shared);
+            }
+            --left;
         }
-    }
-    if (a.x) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i)
+        for (int i = 0; i < NP; ++i) unpack<F32>(r.z[i], z[i]);
+        if (a.post) normed(a.bw, bw, a.bb, bb);
+        if (a.gate || a.scale) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) z[i][e] += x[i][e];
-    }
-    const bool live = at < a.rows;
-    if (a.sum && live) {
+            for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int i = 0; i < NP; ++i) store_piece<F32>((char*)a.sum + row * a.lds * S, piece(i), a.width, z[i]);
-    }
-    if (!a.y) return;
-    // values behind the row's end: the gate and the norm may have left something there
+                for (int e = 0; e < E; ++e) z[i][e] *= gs[i][e];
+        }
+        if (a.x) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
+            for (int i = 0; i < NP; ++i) {
+                float v[E];
+                unpack<F32>(r.x[i], v);
 #pragma unroll
-        for (int e = 0; e < E; ++e) z[i][e] = piece(i) + e < a.width ? z[i][e] : 0.f;
-    normed(a.w, a.b);
-    if (live) {
+                for (int e = 0; e < E; ++e) z[i][e] += v[e];
+            }
+        }
+        const bool live = at < a.rows;
+        if (a.sum && live) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) store_piece<F32>((char*)a.y + row * a.ldy * S, piece(i), a.width, z[i]);
+            for (int i = 0; i < NP; ++i) store_piece<F32>((char*)a.sum + at * a.lds * S, piece(i), a.width, z[i]);
+        }
+        if (!a.y) continue;
+        if (!a.whole) {                                // the norm's bias may have left something behind the row's end
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) z[i][e] = piece(i) + e < a.width ? z[i][e] : 0.f;
+        }
+        normed(a.w, w, a.b, b);
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) store_piece<F32>((char*)a.y + at * a.ldy * S, piece(i), a.width, z[i]);
+        }
     }
 }
 
@@ -278,7 +382,9 @@ __global__ __launch_bounds__(256) void norm_wide_kernel(NormArgs a) {
 
 namespace {
 
-constexpr int NORM_PIECES = 4;                         // at most of a lane
+// Pieces of a lane: three and the rest of the lane's registers is what a wavefront has where a SIMD holds two (rows of
+// 2048 bf16 values, 20000 of them, by four pieces 192 us, by one of a workgroup's lanes 69).
+constexpr int NORM_PIECES = 3, NORM_PIECES_GROUP = 4;
 
 template <bool F32>
 void launch_norm(NormArgs a, hipStream_t s) {
@@ -296,10 +402,14 @@ void launch_norm(NormArgs a, hipStream_t s) {
                 np = n;
             }
         }
-    } else if (pieces <= 256 * NORM_PIECES) {
+    } else if (pieces <= 256 * NORM_PIECES_GROUP) {
         np = (pieces + 255) / 256;
     }
-    const int per = np ? 256 / a.lanes : 1;
+    a.whole = np * a.lanes * (F32 ? 4 : 8) == a.width;
+    // rows of the same lanes, where there are eight wavefronts for each SIMD (four maps: each for itself 243 us, three
+    // 166, eight 147, sixteen 171)
+    a.each = np ? (int)std::min((int64_t)8, std::max((int64_t)1, a.rows * a.lanes / 64 / 4096)) : 1;
+    const int per = np ? 256 / a.lanes * a.each : 1;
     for (int64_t row = 0; row < a.rows; row += LAUNCH_GROUPS * per) {
         a.row0 = row;
         const dim3 grid((unsigned)std::min(LAUNCH_GROUPS, (a.rows - row + per - 1) / per)), block(256);
