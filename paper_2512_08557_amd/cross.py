@@ -10,20 +10,32 @@ from . import tokens as T
 from .engine import _check, lib
 
 
-def _heads(t, name: str, dtype, index: int, dims: int):
+def _heads(t, name: str, dtype, index: int, dims: int) -> int:
     """The row stride of [..., heads, head_dim]: heads one behind the other, rows
     evenly apart, on 16-byte boundaries."""
-    T._require(t, name, dtype, index)
-    if t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} axes as q has")
-    heads, dim = t.shape[-2:]
-    if heads < 1:
-        raise ValueError(f"{name} must have at least one head")
-    if dim > 1 and t.stride(-1) != 1 or heads > 1 and t.stride(-2) != dim:
+    if t.dtype is not dtype or t.get_device() != index:
+        T._require(t, name, dtype, index)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != dims or 0 in shape[-2:]:
+        raise ValueError(f"{name} must have {dims} axes as q has, and at least one head")
+    n, heads, dim = shape[-3:]
+    width = ld = heads * dim
+    if stride[-1] != 1 and dim > 1 or stride[-2] != dim and heads > 1:
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    ld = T._row_stride(t.as_strided(t.shape[:-2] + (heads * dim,), t.stride()[:-2] + (1,)), name, heads * dim)
-    if t.numel() and (t.data_ptr() % 16 or ld * t.element_size() % 16):
-        raise ValueError(f"{name}: its rows must lie on 16-byte boundaries")
+    batch = shape[0] if dims == 4 else 1
+    if n > 0 and batch > 0:
+        if n > 1:
+            ld = stride[-3]
+            if batch > 1 and stride[0] != n * ld:
+                raise ValueError(f"{name}: its rows must lie evenly apart")
+        elif batch > 1:
+            ld = stride[0]
+        if ld < width:
+            raise ValueError(f"{name}: its rows overlap")
+        if t.data_ptr() % 16 or ld * t.element_size() % 16:
+            raise ValueError(f"{name}: its rows must lie on 16-byte boundaries")
+    if t.requires_grad:
+        T._want_gradient()
     return ld
 
 
@@ -51,14 +63,14 @@ def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional
     kind = T._KINDS.get(dtype, -1)
     if kind < 0:
         raise ValueError(f"float32 or bfloat16 tensors, not {dtype}")
-    if not q.is_cuda:
-        raise ValueError("q must be a cuda tensor")
-    if q.dim() not in (3, 4):
-        raise ValueError("q must be [queries, q_heads, head_dim] or [batch, queries, q_heads, head_dim]")
     index, dims = q.get_device(), q.dim()
+    if index < 0:
+        raise ValueError("q must be a cuda tensor")
+    if dims not in (3, 4):
+        raise ValueError("q must be [queries, q_heads, head_dim] or [batch, queries, q_heads, head_dim]")
     ldq = _heads(q, "q", dtype, index, dims)
     ldk, ldv = _heads(k, "k", dtype, index, dims), _heads(v, "v", dtype, index, dims)
-    heads, dim = q.shape[-2:]
+    heads, dim = q.shape[-2], q.shape[-1]
     if k.shape != v.shape or k.shape[-1] != dim or heads % k.shape[-2]:
         raise ValueError("k and v must be of one shape, of q's head_dim and of heads that divide q's")
     if dim not in (32, 64, 128):
@@ -85,8 +97,6 @@ def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional
         if mask.dtype not in (T.torch.bool, T.torch.uint8):
             raise ValueError(f"mask must be bool or uint8, not {mask.dtype}")
         T._dense(mask, "mask", mask.dtype, index, k.shape[:-2])
-    if q.requires_grad or k.requires_grad or v.requires_grad:
-        T._want_gradient()
     if out is None:
         out = q.new_empty(q.shape)
     elif T._dense(out, "out", dtype, index, q.shape) % 16:

@@ -55,23 +55,20 @@ class DeltaMemory:
     def _row(self, t, name: str, tokens: int, heads: int, dim: int) -> int:
         """The stride from token to token of [tokens, heads, dim] (dim 0: [tokens,
         heads]), a token's values contiguous."""
-        shape = (tokens, heads, dim) if dim else (tokens, heads)
-        T._require(t, name, self.kind, self.index, shape)
+        shape, stride = t.shape, t.stride()
+        if t.dtype is not self.kind or t.get_device() != self.index or len(shape) != (3 if dim else 2) or \
+                shape[0] != tokens or shape[1] != heads or (dim and shape[2] != dim):
+            T._require(t, name, self.kind, self.index, (tokens, heads, dim) if dim else (tokens, heads))
         if t.requires_grad:
             T._want_gradient()
-        if dim:
-            if t.stride(2) != 1 or heads > 1 and t.stride(1) != dim:
-                raise ValueError(f"{name}: a token's values must be contiguous")
-            width = heads * dim
-        else:
-            if heads > 1 and t.stride(1) != 1:
-                raise ValueError(f"{name}: a token's values must be contiguous")
-            width = heads
+        if dim and stride[2] != 1 or heads > 1 and stride[1] != (dim or 1):
+            raise ValueError(f"{name}: a token's values must be contiguous")
+        width = heads * (dim or 1)
         if tokens < 2:
             return width
-        if t.stride(0) < width:
+        if stride[0] < width:
             raise ValueError(f"{name}: its tokens overlap")
-        return t.stride(0)
+        return stride[0]
 
     def update(self, q, k, v, a, b, rate=None, bias=None, eps: Optional[float] = 1e-6, scale: Optional[float] = None,
                start=None, max_new: Optional[int] = None, initial=None, out=None, stream=None):
@@ -88,7 +85,7 @@ class DeltaMemory:
         sigmoid(b); without them alpha = exp(a), a <= 0, and beta = b.  scale: 1 /
         sqrt(key_dim) unless given.  initial: states to begin from instead of the
         memory's (which are written all the same)."""
-        torch, index = T.torch, self.index
+        index = self.index
         if q.dim() != 3:
             raise ValueError("q must be [tokens, qk_heads, key_dim]")
         tokens = q.shape[0]
@@ -98,37 +95,37 @@ class DeltaMemory:
             rows = E.TokenRows(tokens, tokens // self.batch, 0, None)
         else:
             rows = E.TokenRows(tokens, tokens if max_new is None else max_new, 0,
-                               T._dense(start, "start", torch.int32, index, (self.batch + 1,)))
-        strides = [self._row(q, "q", tokens, self.qk_heads, self.key_dim),
-                   self._row(k, "k", tokens, self.qk_heads, self.key_dim),
-                   self._row(v, "v", tokens, self.heads, self.value_dim), self._row(a, "a", tokens, self.heads, 0),
-                   self._row(b, "b", tokens, self.heads, 0)]
+                               T._dense(start, "start", T.torch.int32, index, (self.batch + 1,)))
+        heads = self.heads
+        ldq, ldk = self._row(q, "q", tokens, self.qk_heads, self.key_dim), self._row(k, "k", tokens, self.qk_heads, self.key_dim)
+        ldv = self._row(v, "v", tokens, heads, self.value_dim)
+        lda, ldb = self._row(a, "a", tokens, heads, 0), self._row(b, "b", tokens, heads, 0)
         if (rate is None) != (bias is None):
             raise ValueError("rate and bias come together")
         if rate is not None:
             for name, t in (("rate", rate), ("bias", bias)):
-                T._dense(t, name, torch.float32, index, (self.heads,))
+                T._dense(t, name, T.torch.float32, index, (heads,))
                 if t.requires_grad:
                     T._want_gradient()
         if initial is not None:
-            if T._dense(initial, "initial", torch.float32, index, self._state.shape) % 16:
+            if T._dense(initial, "initial", T.torch.float32, index, self._state.shape) % 16:
                 raise ValueError("initial must be on a 16-byte boundary")
             if initial.requires_grad:
                 T._want_gradient()
-        shape = (tokens, self.heads, self.value_dim)
+        shape = (tokens, heads, self.value_dim)
         if out is None:
             out = q.new_empty(shape)
         elif T._dense(out, "out", self.kind, index, shape) % 16:
             raise ValueError("out must be on a 16-byte boundary")
         spec = E.DeltaSpec(0 if eps is None else 1, 0.0 if eps is None else eps,
-                           self.key_dim ** -0.5 if scale is None else scale, *strides)
+                           self.key_dim ** -0.5 if scale is None else scale, ldq, ldk, ldv, lda, ldb)
         need, work = ctypes.c_size_t(), None
         _check(lib().sscater_delta_workspace(spec, self._spec, rows, need), "sscater_delta_workspace")
         if need.value:
-            work = q.new_empty(need.value, dtype=torch.uint8)
-        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+            work = q.new_empty(need.value, dtype=T.torch.uint8)
         T._launch(lib().sscater_delta_update, "sscater_delta_update", index, stream,
-                  (q, k, v, a, b, rate, bias, initial, start, out, work, self._state), spec, self._spec, rows, ptr(initial),
-                  q.data_ptr(), k.data_ptr(), v.data_ptr(), a.data_ptr(), b.data_ptr(), ptr(rate), ptr(bias),
-                  out.data_ptr(), ptr(work), need.value)
+                  (q, k, v, a, b, rate, bias, initial, start, out, work, self._state), spec, self._spec, rows,
+                  None if initial is None else initial.data_ptr(), q.data_ptr(), k.data_ptr(), v.data_ptr(), a.data_ptr(),
+                  b.data_ptr(), None if rate is None else rate.data_ptr(), None if bias is None else bias.data_ptr(),
+                  out.data_ptr(), None if work is None else work.data_ptr(), need.value)
         return out

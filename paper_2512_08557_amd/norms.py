@@ -13,21 +13,33 @@ GATES = {None: 0, "none": 0, "silu": 3, "sigmoid": 4}
 
 
 def _width(t, name: str, dtype, index: int, width: int):
-    T._require(t, name, dtype, index, (width,))
-    if width > 1 and t.stride(0) != 1:
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != index or t.dim() != 1 or t.shape[0] != width:
+        T._require(t, name, dtype, index, (width,))
+    if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    if t.requires_grad:
+        T._want_gradient()
     return t.data_ptr()
 
 
-def _gate(gate, activation, x, dtype, index: int, rows: int):
-    """The gate's row stride, and how many rows of x share one of its rows: its
-    shape is x's without some of the axes before the last."""
+def _rows(t, name: str, dtype, index: int, shape, width: int) -> int:
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        T._require(t, name, dtype, index, shape)
+    if t.requires_grad:
+        T._want_gradient()
+    return width if t.is_contiguous() else T._row_stride(t, name, width)
+
+
+def _gate(gate, dtype, index: int, shape, width: int, rows: int):
+    """The gate's row stride, and how many rows share one of its rows: its shape is
+    the rows' without some of the axes before the last."""
     lead = gate.dim() - 1
-    if lead < 0 or lead > x.dim() - 1 or gate.shape[:-1] != x.shape[:lead] or gate.shape[-1] != x.shape[-1]:
-        raise ValueError(f"gate must be {tuple(x.shape)} or that without axes before the last, not {tuple(gate.shape)}")
-    T._require(gate, "gate", dtype, index)
-    n = gate.numel() // x.shape[-1]
-    return T._row_stride(gate, "gate", x.shape[-1]), rows // n if n else 1
+    if lead < 0 or lead > len(shape) - 1 or gate.shape[:-1] != shape[:lead] or gate.shape[-1] != width:
+        raise ValueError(f"gate must be {tuple(shape)} or that without axes before the last, not {tuple(gate.shape)}")
+    n = gate.numel() // width
+    return _rows(gate, "gate", dtype, index, gate.shape, width), max(rows // n if n else 1, 1)
 
 
 def _call(x, block, block_norm, block_weight, block_bias, gate, activation, scale, weight, bias, eps, center, total, y,
@@ -40,34 +52,28 @@ def _call(x, block, block_norm, block_weight, block_bias, gate, activation, scal
     dtype, shape, index = block.dtype, block.shape, block.get_device()
     width = shape[-1]
     rows = block.numel() // width
-    stride = {"block": T._row_stride(block, "block" if x is not None else "x", width)}
-    for name, t in (("x", x), ("total", total), ("out", y)):
-        if t is not None:
-            stride[name] = T._row_stride(T._require(t, name, dtype, index, shape), name, width)
-    shared = 1
-    if gate is not None:
-        stride["gate"], shared = _gate(gate, activation, block, dtype, index, rows)
-    vectors = (block_weight, block_bias, scale, weight, bias)
-    at = [None if t is None else _width(t, name, dtype, index, width)
-          for name, t in zip(("block_weight", "block_bias", "scale", "weight", "bias"), vectors)]
-    for t in (x, block, gate) + vectors:
-        if t is not None and t.requires_grad:
-            T._want_gradient()
-    spec = E.NormSpec(rows, max(shared, 1), width, T._KINDS[dtype], 1 if center else 0, 1 if block_norm else 0, act, eps,
-                      stride.get("x", width), stride["block"], stride.get("gate", width), stride.get("total", width),
-                      stride.get("out", width))
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    T._launch(lib().sscater_norm, "sscater_norm", index, stream, (x, block, gate, total, y) + vectors, spec, ptr(x),
-              block.data_ptr(), at[0], at[1], ptr(gate), at[2], at[3], at[4], ptr(total), ptr(y))
+    ldb = _rows(block, "block" if x is not None else "x", dtype, index, shape, width)
+    ldx = width if x is None else _rows(x, "x", dtype, index, shape, width)
+    lds = _rows(total, "total", dtype, index, shape, width)
+    ldy = width if y is None else _rows(y, "out", dtype, index, shape, width)
+    ldg, shared = (width, 1) if gate is None else _gate(gate, dtype, index, shape, width, rows)
+    spec = E.NormSpec(rows, shared, width, T._KINDS[dtype], 1 if center else 0, 1 if block_norm else 0, act, eps, ldx, ldb,
+                      ldg, lds, ldy)
+    T._launch(lib().sscater_norm, "sscater_norm", index, stream,
+              (x, block, gate, total, y, block_weight, block_bias, scale, weight, bias), spec,
+              None if x is None else x.data_ptr(), block.data_ptr(), _width(block_weight, "block_weight", dtype, index, width),
+              _width(block_bias, "block_bias", dtype, index, width), None if gate is None else gate.data_ptr(),
+              _width(scale, "scale", dtype, index, width), _width(weight, "weight", dtype, index, width),
+              _width(bias, "bias", dtype, index, width), total.data_ptr(), None if y is None else y.data_ptr())
 
 
 def _tensor(t, name: str) -> None:
     if T.torch is None:
         T._bind()
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a cuda tensor")
     if t.dtype not in T._KINDS:
         raise ValueError(f"float32 or bfloat16 tensors, not {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a cuda tensor")
     if t.dim() < 1 or t.shape[-1] < 1:
         raise ValueError(f"{name} must be [..., width], of at least one value")
 
@@ -96,7 +102,6 @@ def add_norm(x, block, weight=None, bias=None, *, block_weight=None, block_bias=
     out [..., width], gate as for norm(), the rest [width].  total may be x or block, out
     too (not both the same); otherwise they overlap nothing."""
     _tensor(block, "block")
-    T._require(x, "x", block.dtype, block.get_device(), block.shape)
     if weight is None and (bias is not None or out is not None):
         raise ValueError("bias and out come with weight")
     if block_weight is None and block_bias is not None:
@@ -105,7 +110,7 @@ def add_norm(x, block, weight=None, bias=None, *, block_weight=None, block_bias=
         total = block.new_empty(block.shape)
     if out is None and weight is not None:
         out = block.new_empty(block.shape)
-    if out is not None and block.numel() and out.data_ptr() == total.data_ptr():
+    if out is not None and out.data_ptr() == total.data_ptr() and block.numel():
         raise ValueError("total and out must be two tensors")
     _call(x, block, block_weight is not None, block_weight, block_bias, gate, activation, scale, weight, bias, eps, center,
           total, out, stream)
