@@ -19,7 +19,7 @@ bool attend_cut(const sscater_attend_spec* s, const sscater_token_cache* c, cons
     if (r->tokens > 0 && c->capacity - c->sinks < reach) return false;
     const int64_t rows = (int64_t)r->max_new * (s->q_heads / c->kv_heads);
     if (rows > (1 << 30) || (int64_t)r->tokens * s->q_heads > (int64_t(1) << 40)) return false;
-    cut_keys(cut, c->dtype == SSCATER_F32, c->head_dim, rows, (int64_t)c->kv_heads * c->batch, reach + c->sinks);
+    cut_keys(cut, c->dtype == SSCATER_F32, c->head_dim, rows, (int64_t)c->kv_heads * c->batch, reach + c->sinks, false);
     return cut->grid <= 0x7FFFFFFF;
 }
 

@@ -777,8 +777,9 @@ struct AttendCut {
     int64_t grid;
 };
 
-// rows: of a sequence and key head, at most; heads: key heads of all sequences; keys: of a sequence, at most
-inline void cut_keys(AttendCut* cut, bool f32, int dim, int64_t rows, int64_t heads, int64_t keys) {
+// rows: of a sequence and key head, at most; heads: key heads of all sequences; keys: of a sequence, at most; uneven:
+// sequences may be much shorter than that
+inline void cut_keys(AttendCut* cut, bool f32, int dim, int64_t rows, int64_t heads, int64_t keys, bool uneven) {
     // fp32 heads of 128 values: two tiles of keys and of values for each of four wavefronts would not fit
     cut->wm = rows <= 32 && !(f32 && dim == 128) ? 1 : rows <= 64 ? 2 : 4;
     cut->qtiles = (int)((rows + 32 * cut->wm - 1) / (32 * cut->wm));
@@ -802,6 +803,9 @@ inline void cut_keys(AttendCut* cut, bool f32, int dim, int64_t rows, int64_t he
                 cut->splits = (int)n;
             }
         }
+        // Of sequences whose lengths only the device knows the longest would be the time: three times as many workgroups as
+        // places, so that the short ones' make room.
+        if (uneven) cut->splits = (int)std::max((int64_t)cut->splits, std::min((3 * places + base - 1) / base, most));
     }
     cut->grid = base * cut->splits;
 }

@@ -13,28 +13,17 @@
 
 namespace ssc {
 
-constexpr int LIST_KEYS = 16384;                       // of a workgroup: sixteen each of 1024 threads
+constexpr int LIST_KEYS = 4096;                        // of a workgroup: four each of 1024 threads
 
-// Visible keys among sixteen of a mask from `at` on, of n: a bit for each byte that is not zero.
-__device__ __forceinline__ uint32_t seen16(const uint8_t* mask, int at, int n) {
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (at + 16 <= n) {
-        __builtin_memcpy(w, mask + at, 16);
-    } else {
-        for (int i = 0; at + i < n && i < 16; ++i) w[i >> 2] |= (uint32_t)mask[at + i] << (8 * (i & 3));
-    }
-    uint32_t bits = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t x = (((w[i] & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w[i]) & 0x80808080u;
-        bits |= ((x * 0x00204081u) >> 28 & 15u) << (4 * i);
-    }
-    return bits;
+// Which bytes of a word are not zero, a bit each.
+__device__ __forceinline__ uint32_t seen4(uint32_t w) {
+    const uint32_t x = (((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) & 0x80808080u;
+    return x * 0x00204081u >> 28;
 }
 
 // A sequence's visible keys in order.  Workgroup b * parts + p lists those among the p-th
-// LIST_KEYS of sequence b, behind the ones before them, which it counts itself: a second
-// launch would take longer than reading a mask again.
+// LIST_KEYS of sequence b, behind the ones before them, which it counts itself, 16 bytes a
+// lane: a second launch would take longer than reading a mask again.
 __global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRows keys, int32_t* list, int32_t* count,
                                                     int parts, int64_t id0) {
     __shared__ int sums[2][16];
@@ -42,13 +31,25 @@ __global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRo
     const int b = (int)(id / parts), t = threadIdx.x;
     int first, n;
     rows_of(keys, b, first, n);
-    const int part = (int)(id % parts) * LIST_KEYS;
+    const int part = (int)(id % parts) * LIST_KEYS, at = part + 4 * t;
     if (part >= n && part > 0) return;
     mask += first;
+    uint32_t word = 0;
+    if (at + 4 <= n) {
+        __builtin_memcpy(&word, mask + at, 4);
+    } else {
+        for (int i = 0; at + i < n; ++i) word |= (uint32_t)mask[at + i] << (8 * i);
+    }
     int before = 0;
-    for (int at = t * 16; at < part; at += LIST_KEYS) before += __popc(seen16(mask, at, n));
-    uint32_t bits = part + t * 16 < n ? seen16(mask, part + t * 16, n) : 0;
-    int mine = __popc(bits), upto = mine;
+#pragma unroll 4
+    for (int i = t * 16; i < part; i += 16 * 1024) {
+        uint32_t w[4];
+        __builtin_memcpy(w, mask + i, 16);
+        before += __popc(seen4(w[0])) + __popc(seen4(w[1])) + __popc(seen4(w[2])) + __popc(seen4(w[3]));
+    }
+    const uint32_t bits = seen4(word);
+    const int mine = __popc(bits);
+    int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
         before += __shfl_xor(before, o);
@@ -67,10 +68,9 @@ __global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRo
         all += sums[0][w] + sums[1][w];
     }
     int32_t* to = list + first + base + upto - mine;
-    while (bits) {
-        *to++ = part + t * 16 + __ffs(bits) - 1;
-        bits &= bits - 1;
-    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (bits >> i & 1) *to++ = at + i;
     if (t == 0 && part + LIST_KEYS >= n) count[b] = all;
 }
 
@@ -101,7 +101,8 @@ bool cross_plan(const sscater_cross_spec* s, bool masked, CrossPlan* p) {
         return false;
     const int64_t rows = (int64_t)s->max_q * (s->q_heads / s->kv_heads);
     if (rows > (1 << 30) || (int64_t)s->queries * s->q_heads > (int64_t(1) << 40)) return false;
-    cut_keys(&p->cut, s->dtype == SSCATER_F32, s->head_dim, rows, (int64_t)s->kv_heads * s->batch, s->max_k);
+    cut_keys(&p->cut, s->dtype == SSCATER_F32, s->head_dim, rows, (int64_t)s->kv_heads * s->batch, s->max_k,
+             s->batch > 1 && s->q_start != nullptr);
     if (p->cut.grid > 0x7FFFFFFF) return false;
     p->part = p->cut.splits > 1 ? (size_t)p->cut.splits * s->queries * s->q_heads * (s->head_dim + 2) * 4 : 0;
     p->part = (p->part + 15) / 16 * 16;
