@@ -7,7 +7,8 @@
 // (columns do not depend on one another).  Lane 8 c + r holds the r-th eighth of the
 // rows of columns 4 c .. 4 c + 3, so a product with the state is key_dim / 2
 // multiplications a lane and a sum between eight neighbouring lanes, and q and k come
-// as one run of values for each lane.
+// as one run of values for each lane.  alpha and beta are formed for 64 tokens at a time,
+// a token a lane.
 //
 // Stretches of 64 tokens at once: with G the running sum of log(alpha) within one, the
 // corrections u are the solution of a triangular system that no state is in,
@@ -27,6 +28,7 @@
 #include "tokens.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace ssc {
@@ -131,21 +133,25 @@ __global__ __launch_bounds__(256) void delta_token_kernel(DeltaArgs a) {
     const bool raw = a.rate != nullptr;
     const float rate = raw ? a.rate[h] : 0.f, bias = raw ? a.bias[h] : 0.f;
     struct Token {
-        float q[R], k[R], v[4], a, b;
+        float q[R], k[R], v[4];
     };
     auto fetch = [&](int64_t t) __attribute__((always_inline)) {
         Token x;
         values_at<F32>(a.q, t * a.ldq + hk * DK + r0, x.q);
         values_at<F32>(a.k, t * a.ldk + hk * DK + r0, x.k);
         values_at<F32>(a.v, t * a.ldv + h * DV + c0, x.v);
-        x.a = value_at<F32>(a.a, t * a.lda + h);
-        x.b = value_at<F32>(a.b, t * a.ldb + h);
         return x;
     };
     Token next;
     if (n > 0) next = fetch(first);
+    float alphas = 0.f, betas = 0.f;
     for (int i = 0; i < n; ++i) {
         const int64_t t = first + i;
+        if (i % 64 == 0) {
+            const int64_t mine = t + min(lane, n - 1 - i);
+            alphas = expf(log_alpha(value_at<F32>(a.a, mine * a.lda + h), rate, bias, raw));
+            betas = beta_of(value_at<F32>(a.b, mine * a.ldb + h), raw);
+        }
         Token x = next;
         if (i + 1 < n) next = fetch(t + 1);
         float fq = a.scale, fk = 1.f;
@@ -156,10 +162,11 @@ __global__ __launch_bounds__(256) void delta_token_kernel(DeltaArgs a) {
                 qq = fmaf(x.q[j], x.q[j], qq);
                 kk = fmaf(x.k[j], x.k[j], kk);
             }
-            fq *= 1.f / sqrtf(sum8(qq) + a.eps);
-            fk = 1.f / sqrtf(sum8(kk) + a.eps);
+            fq *= __builtin_amdgcn_rsqf(sum8(qq) + a.eps);
+            fk = __builtin_amdgcn_rsqf(sum8(kk) + a.eps);
         }
-        const float alpha = expf(log_alpha(x.a, rate, bias, raw)), beta = beta_of(x.b, raw);
+        const float alpha = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(alphas), i % 64)),
+                    beta = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(betas), i % 64));
         f4v p = {0.f, 0.f, 0.f, 0.f}, o = {0.f, 0.f, 0.f, 0.f}, u;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -409,6 +416,9 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     constexpr int S = F32 ? 4 : 2;
     constexpr int NT = DK / 16, OWN = (NT + 3) / 4;    // row tiles of the state, and those of a wavefront
     __shared__ __attribute__((aligned(16))) f4v sbuf[NT][64], zbuf[NT][64], xbuf[4][64], ubuf[4][64];
+    // the stretch's keys, for their transpose: rows of fp32 values, whose same columns four rows further on are 16 banks on
+    constexpr int PITCH = DK + 4;
+    __shared__ __attribute__((aligned(16))) float kbuf[CHUNK][PITCH];
     __shared__ float part[2][16][16];
     __shared__ uint32_t bad[4];
     // the columns of a head follow one another on one XCD (workgroup id mod 8), whose L2 then has its keys and matrices
@@ -432,7 +442,11 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     auto b_of = [&](int j, int tile) __attribute__((always_inline)) {
         return (f4v*)(part0 + j * PART + DK * DK + ((int64_t)tile * (DV / 16) + block) * 256 + lane * 4);
     };
-    const float* const mat = mats + ((int64_t)slot_of(first, b) * a.heads + h) * MATS;
+    // of the stretch whose operands are loaded next, moved on from one to the next: a stretch's worth of scalar
+    // multiplications is time on every wavefront's way
+    const int64_t row0 = first + (int64_t)c0 * CHUNK, step_m = (int64_t)a.heads * MATS;
+    const float* mx = mats + ((int64_t)(slot_of(first, b) + c0) * a.heads + h) * MATS;
+    const float *mu = mx, *ms = mx;
     const uint32_t ldk = (uint32_t)a.ldk * S, ldq = (uint32_t)a.ldq * S, ldv = (uint32_t)a.ldv * S;
     auto tokens = [&](int c) __attribute__((always_inline)) { return min(CHUNK, n - c * CHUNK); };
     auto put = [&](int64_t t, float v) __attribute__((always_inline)) {
@@ -450,24 +464,26 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         Raw4<F32> q[NT];
         f4v p[4], fq;
         uint32_t off = (uint32_t)(16 * wq + r) * ldq + 4 * g * S;
+        const char* at = (const char*)a.q + (row0 * a.ldq + hk * DK) * S;
+        const int64_t step_q = (int64_t)CHUNK * ldq;
         auto load_q = [&](int c) __attribute__((always_inline)) {
-            const int64_t t0 = first + (int64_t)c * CHUNK;
-            const char* const at = (const char*)a.q + (t0 * a.ldq + hk * DK) * S;
             const int m = tokens(c);
             if (m < CHUNK) off = (uint32_t)min(16 * wq + r, m - 1) * ldq + 4 * g * S;
 #pragma unroll
             for (int t = 0; t < NT; ++t) q[t].load(at + off + 16 * t * S, 0);
-            fq = *(const f4v*)&mat[(int64_t)c * a.heads * MATS + MATS_TOKEN + TOKEN_Q * CHUNK + 16 * wq + 4 * g];
+            fq = *(const f4v*)&mx[MATS_TOKEN + TOKEN_Q * CHUNK + 16 * wq + 4 * g];
         };
-        auto load_p = [&](int c) __attribute__((always_inline)) {
+        const uint32_t off_p = (MATS_P + lower(wq, 0) * 256 + lane * 4) * 4;
+        auto load_p = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                p[i] = *(const f4v*)&mat[(int64_t)c * a.heads * MATS + MATS_P + lower(wq, min(i, wq)) * 256 + lane * 4];
+            for (int i = 0; i < 4; ++i) p[i] = *(const f4v*)((const char*)mu + off_p + (uint32_t)min(i, wq) * 1024);
         };
         if (chunks > c0) {
             load_q(c0);
-            load_p(c0);
+            load_p();
         }
+        const int64_t out_row = (int64_t)a.heads * DV;
+        char* to = (char*)a.out + ((row0 + 16 * wq + 4 * g) * out_row + h * DV + col) * S;
         lds_barrier();
         for (int j = 1; j < seg; ++j) {
             lds_barrier();
@@ -488,17 +504,27 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
                 o[0][e] = (o[0][e] + o[1][e]) * fq[e];
                 o[1][e] = 0.f;
             }
+            if (c + 1 < chunks) {
+                at += step_q;
+                mx += step_m;
+            }
             load_q(next);
             lds_barrier();
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 if (t <= wq) o[t & 1] = tile_product(p[t], ubuf[t][lane], o[t & 1]);
-            load_p(next);
+            if (c + 1 < chunks) mu += step_m;
+            load_p();
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int t = 16 * wq + 4 * g + e;
-                if (t < m && !(columns >> r & 1)) put(first + (int64_t)c * CHUNK + t, o[0][e] + o[1][e]);
+                const float v = o[0][e] + o[1][e];
+                char* const at = to + e * out_row * S;
+                if (16 * wq + 4 * g + e < m && !(columns >> r & 1)) {
+                    if constexpr (F32) *(float*)at = v;
+                    else *(uint16_t*)at = (uint16_t)bf16_pair(v, v);
+                }
             }
+            to += CHUNK * out_row * S;
             lds_barrier();
         }
         return;
@@ -526,23 +552,17 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         if (own) sbuf[tile(o)][lane] = s[o];
     }
     Raw4<F32> k[NT];
-    Raw1<F32> kt[OWN][4][4], v[4];
+    Raw1<F32> v[4];
     f4v inv[4], fk, fb, fu[4];
     float last, keys_odd;
-    uint32_t off_k = (uint32_t)(16 * w + r) * ldk + 4 * g * S, off_t[4][4], off_v[4];
+    uint32_t off_k = (uint32_t)(16 * w + r) * ldk + 4 * g * S, off_v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        off_v[e] = (uint32_t)(16 * w + 4 * g + e) * ldv + col * S;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) off_t[t][e] = (uint32_t)(16 * t + 4 * g + e) * ldk + (16 * tile(0) + r) * S;
-    }
-    auto keys_of = [&](int c) __attribute__((always_inline)) {
-        return (const char*)a.k + ((first + (int64_t)c * CHUNK) * a.ldk + hk * DK) * S;
-    };
+    for (int e = 0; e < 4; ++e) off_v[e] = (uint32_t)(16 * w + 4 * g + e) * ldv + col * S;
+    const char* keys = (const char*)a.k + (row0 * a.ldk + hk * DK) * S;
+    const char* values = (const char*)a.v + (row0 * a.ldv + h * DV) * S;
+    const int64_t step_k = (int64_t)CHUNK * ldk, step_v = (int64_t)CHUNK * ldv;
     // (the rows behind a stream's last token are that token once more)
     auto load_x = [&](int c) __attribute__((always_inline)) {
-        const char* const at = (const char*)a.v + ((first + (int64_t)c * CHUNK) * a.ldv + h * DV) * S;
-        const float* const mc = mat + (int64_t)c * a.heads * MATS;
         const int m = tokens(c);
         if (m < CHUNK) {
             off_k = (uint32_t)min(16 * w + r, m - 1) * ldk + 4 * g * S;
@@ -550,35 +570,22 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             for (int e = 0; e < 4; ++e) off_v[e] = (uint32_t)min(16 * w + 4 * g + e, m - 1) * ldv + col * S;
         }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) k[t].load(keys_of(c) + off_k + 16 * t * S, 0);
+        for (int t = 0; t < NT; ++t) k[t].load(keys + off_k + 16 * t * S, 0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e].load(at + off_v[e], 0);
-        fk = *(const f4v*)&mc[MATS_TOKEN + TOKEN_K * CHUNK + 16 * w + 4 * g];
-        fb = *(const f4v*)&mc[MATS_TOKEN + TOKEN_BETA * CHUNK + 16 * w + 4 * g];
-        keys_odd = mc[MATS_LAST + 1];
+        for (int e = 0; e < 4; ++e) v[e].load(values + off_v[e], 0);
+        fk = *(const f4v*)&mx[MATS_TOKEN + TOKEN_K * CHUNK + 16 * w + 4 * g];
+        fb = *(const f4v*)&mx[MATS_TOKEN + TOKEN_BETA * CHUNK + 16 * w + 4 * g];
+        keys_odd = mx[MATS_LAST + 1];
     };
-    auto load_u = [&](int c) __attribute__((always_inline)) {
+    const uint32_t off_m = (lower(w, 0) * 256 + lane * 4) * 4;
+    auto load_u = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) inv[i] = *(const f4v*)&mat[(int64_t)c * a.heads * MATS + lower(w, min(i, w)) * 256 + lane * 4];
+        for (int i = 0; i < 4; ++i) inv[i] = *(const f4v*)((const char*)mu + off_m + (uint32_t)min(i, w) * 1024);
     };
-    auto load_s = [&](int c) __attribute__((always_inline)) {
-        const float* const mc = mat + (int64_t)c * a.heads * MATS;
-        const int m = tokens(c);
-        if (m < CHUNK) {
+    auto load_s = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) off_t[t][e] = (uint32_t)min(16 * t + 4 * g + e, m - 1) * ldk + (16 * tile(0) + r) * S;
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-#pragma unroll
-            for (int o = 0; o < OWN; ++o)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) kt[o][t][e].load(keys_of(c) + off_t[t][e] + 64 * o * S, 0);
-            fu[t] = *(const f4v*)&mc[MATS_TOKEN + TOKEN_U * CHUNK + 16 * t + 4 * g];
-        }
-        last = mc[MATS_LAST];
+        for (int t = 0; t < 4; ++t) fu[t] = *(const f4v*)&ms[MATS_TOKEN + TOKEN_U * CHUNK + 16 * t + 4 * g];
+        last = ms[MATS_LAST];
     };
     // Tokens one by one, for columns with infinities or NaN in a stretch (all of them, if in its keys or gates): a product
     // with a triangle's zeros would carry them to the tokens before.  Thread 16 p + column has the p-th sixteenth of a
@@ -636,8 +643,8 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     };
     if (chunks > c0) {
         load_x(c0);
-        load_u(c0);
-        load_s(c0);
+        load_u();
+        load_s();
     }
     lds_barrier();
     if constexpr (OUT) {
@@ -666,7 +673,11 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         // two sums: an instruction need not wait for the one before it
         f4v x[2] = {};
 #pragma unroll
-        for (int t = 0; t < NT; ++t) x[t & 1] = tile_product(k[t].get(), sbuf[t][lane], x[t & 1]);
+        for (int t = 0; t < NT; ++t) {
+            const f4v key = k[t].get();
+            *(f4v*)&kbuf[16 * w + r][16 * t + 4 * g] = key;
+            x[t & 1] = tile_product(key, sbuf[t][lane], x[t & 1]);
+        }
         bool odd = keys_odd != 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -677,10 +688,22 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         xbuf[w][lane] = x[0];
         const uint64_t lanes = __ballot(odd);
         if (lane == 0) bad[w] = (uint32_t)(lanes | lanes >> 32) | (uint32_t)(lanes >> 16 | lanes >> 48);
+        if (c + 1 < chunks) {
+            keys += step_k;
+            values += step_v;
+            mx += step_m;
+        }
         load_x(next);
         lds_barrier();
         const uint32_t columns = bad_columns();
         if (columns) slowly(c, columns);
+        f4v kt[OWN][4];
+#pragma unroll
+        for (int i = 0; i < OWN; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kt[i][t][e] = kbuf[16 * t + 4 * g + e][16 * tile(i) + r];
         f4v u[2] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -690,7 +713,8 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         for (int i = 0; i < OWN; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[i][e] *= last;
-        load_u(next);
+        if (c + 1 < chunks) mu += step_m;
+        load_u();
         lds_barrier();
         f4v more[OWN] = {};
 #pragma unroll
@@ -700,9 +724,8 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             for (int e = 0; e < 4; ++e) y[e] *= fu[t][e];
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
-                const f4v key = {kt[i][t][0].get(), kt[i][t][1].get(), kt[i][t][2].get(), kt[i][t][3].get()};
-                if (t & 1) more[i] = tile_product(key, y, more[i]);
-                else s[i] = tile_product(key, y, s[i]);
+                if (t & 1) more[i] = tile_product(kt[i][t], y, more[i]);
+                else s[i] = tile_product(kt[i][t], y, s[i]);
             }
         }
 #pragma unroll
@@ -711,7 +734,8 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             if (columns >> r & 1) s[i] = zbuf[tile(i)][lane];
             if (own) sbuf[tile(i)][lane] = s[i];
         }
-        load_s(next);
+        if (c + 1 < chunks) ms += step_m;
+        load_s();
         lds_barrier();
     }
     if (!own) return;
@@ -734,9 +758,6 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
 
 namespace {
 
-// Whether a call's tokens are taken in stretches.
-bool in_chunks(const sscater_token_rows* r) { return r->max_new >= 32; }
-
 constexpr int MAX_PARTS = 64;
 
 // Stretches of a call, parts of a stream and the stretches of a part; no stretches: tokens one by one.
@@ -753,23 +774,29 @@ void launch_chunks(DeltaArgs a, int64_t slots, float* mats, hipStream_t s) {
     }
 }
 
-// Parts of the streams: what makes both launches' rounds over the card shortest.  In microseconds, measured at heads of
-// 64 x 64: a stretch with its outputs 2.5 and without 1.6, a product of parts 0.8, a launch and its first loads 5.
+// Tokens one by one or in stretches, and the parts of the streams: whichever takes least by what the pieces take, in
+// microseconds.  A token is 0.35 and 0.0055 for each row of a head's state, or 0.45 for each thousand wavefronts where
+// there are many; a stretch with its outputs 2.5, without 1.6 (two workgroups on a compute unit), a product of parts 0.8; a
+// launch of states 1.5 for each round over the card, chunk_kernel 1 for 150 heads' stretches; the further launches 5 each.
+// (Heads of 64 x 64 in bf16, one by one and in stretches: 8 heads, 4 tokens 7.4 and 13.5, 16 tokens 16.0 and 13.6, 64
+// tokens 49 and 14; 128 heads, 16 tokens 16.4 and 19.0, 32 tokens 28 and 20; 8000 heads, 64 tokens 462 and 789, 128 tokens
+// 895 and 1114; 2400 heads of 32 x 32, 64 tokens 77 and 125.)
 DeltaPlan delta_plan(const sscater_delta_memory* m, const sscater_token_rows* r) {
     DeltaPlan p = {0, 1, 0};
-    if (!in_chunks(r)) return p;
-    p.slots = (int64_t)r->tokens / CHUNK + m->batch;
-    const int64_t heads = (int64_t)m->batch * m->heads, most = (r->max_new + CHUNK - 1) / CHUNK;
-    double best = 0.;
-    for (int64_t n = 1; n <= std::min(most, (int64_t)MAX_PARTS); ++n) {
-        const int64_t length = (most + n - 1) / n, out = heads * (m->value_dim / 16) * n,
-                      in = heads * ((m->value_dim + m->key_dim) / 16) * (n - 1);
-        if ((most + length - 1) / length != n || (n > 1 && out > 2048)) continue;
-        const double cost = length * (2.5 * ((out + 255) / 256) + (n > 1 ? 1.6 * ((in + 511) / 512) : 0.)) +
-                            (n > 1 ? 5. + 0.8 * (n - 2) : 0.);
-        if (n == 1 || cost < best) {
+    const double heads = (double)m->batch * m->heads, n = r->max_new, blocks = m->value_dim / 16;
+    const double token = 5. + n * std::max(0.35 + 0.0055 * m->key_dim, 0.00045 * heads * blocks / 2.);
+    const int64_t most = ((int64_t)r->max_new + CHUNK - 1) / CHUNK;
+    double best = token;
+    for (int64_t k = 1; k <= std::min(most, (int64_t)MAX_PARTS); ++k) {
+        const int64_t length = (most + k - 1) / k;
+        const double out = std::ceil(heads * blocks * k / 256.), in = std::ceil(heads * (blocks + m->key_dim / 16) * (k - 1) / 512.);
+        if ((most + length - 1) / length != k || (k > 1 && out > 8.)) continue;
+        const double cost = 8. + heads * most / 150. + out * (1.5 + 2.5 * length) +
+                            (k > 1 ? 5. + in * (1.5 + 1.6 * length) + 0.8 * (k - 2) : 0.);
+        if (cost < best) {
             best = cost;
-            p.parts = (int)n;
+            p.slots = (int64_t)r->tokens / CHUNK + m->batch;
+            p.parts = (int)k;
             p.length = (int)length;
         }
     }
