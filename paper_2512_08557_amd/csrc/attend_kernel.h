@@ -187,7 +187,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     if (tile * C::BM >= nr) return;
     const int64_t past = CACHE ? past_of(a.rows, b) : 0;
     Reach reach;
-    int k_first = 0;                               // ROWS, LISTED: the sequence's first row
+    int k_first = 0, k_last = 0;                   // ROWS, LISTED: the sequence's first row, and its last from there
     if constexpr (CACHE) {
         const int i0 = tile * C::BM / a.group, i1 = (min((tile + 1) * C::BM, nr) - 1) / a.group;
         reach.lo = max((int64_t)0, (a.causal ? past + i0 : past) - a.window + 1);
@@ -202,6 +202,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         int kn;
         rows_of(TokenRows{a.keys, a.max_k, a.rows.batch, a.k_start, nullptr}, b, k_first, kn);
         reach.total = LISTED ? min(a.count[b], kn) : kn;
+        k_last = kn - 1;
     }
     const int row = min(tile * C::BM + wm * 32 + col, nr - 1);
     const int tok = row / a.group;
@@ -283,7 +284,8 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     };
     // row r of tile t, of round j, which need not be whole
     auto row_of = [&](int t, int j, int r) __attribute__((always_inline)) -> int64_t {
-        if constexpr (LISTED) return named[wk][j & 3][r];
+        // (sequences that overlap, against the call's contract, write over one another's lists)
+        if constexpr (LISTED) return min(named[wk][j & 3][r], k_last);
         const int u = min(t * C::BN + r, reach.total - 1);
         if constexpr (CACHE) return slot_of(a, reach, u);
         return u;
@@ -615,7 +617,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
             if ((u / C::BN - tb) % C::WK != wk || !(u <= last && (u >= from || u < a.sinks))) continue;
             int64_t at = u;
             if constexpr (CACHE) at = slot_of(a, reach, u);
-            if constexpr (LISTED) at = a.list[k_first + u];
+            if constexpr (LISTED) at = min(a.list[k_first + u], k_last);
             float x = 0.f;
 #pragma unroll 1
             for (int c = 0; c < C::RB / 16; ++c) {

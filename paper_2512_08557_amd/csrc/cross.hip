@@ -79,7 +79,8 @@ namespace {
 // What a call needs of its workspace: the splits' sums, the lists, their lengths.
 struct CrossPlan {
     AttendCut cut;
-    size_t part, list, all;
+    int queries, keys;     // rows that the sequences can have
+    size_t list, all;
 };
 
 bool cross_plan(const sscater_cross_spec* s, bool masked, CrossPlan* p) {
@@ -104,10 +105,11 @@ bool cross_plan(const sscater_cross_spec* s, bool masked, CrossPlan* p) {
     cut_keys(&p->cut, s->dtype == SSCATER_F32, s->head_dim, rows, (int64_t)s->kv_heads * s->batch, s->max_k,
              s->batch > 1 && s->q_start != nullptr);
     if (p->cut.grid > 0x7FFFFFFF) return false;
-    p->part = p->cut.splits > 1 ? (size_t)p->cut.splits * s->queries * s->q_heads * (s->head_dim + 2) * 4 : 0;
-    p->part = (p->part + 15) / 16 * 16;
-    p->list = p->part;
-    p->all = masked && s->keys > 0 ? p->list + ((size_t)s->keys + s->batch) * 4 : p->part;
+    p->queries = (int)std::min((int64_t)s->queries, (int64_t)s->max_q * s->batch);
+    p->keys = (int)std::min((int64_t)s->keys, (int64_t)s->max_k * s->batch);
+    p->list = p->cut.splits > 1 ? (size_t)p->cut.splits * p->queries * s->q_heads * (s->head_dim + 2) * 4 : 0;
+    p->list = (p->list + 15) / 16 * 16;
+    p->all = p->list + (masked && p->keys > 0 ? ((size_t)p->keys + s->batch) * 4 : 0);
     return true;
 }
 
@@ -156,16 +158,16 @@ int sscater_cross_attend(const sscater_cross_spec* spec, const void* q, const vo
                          const uint8_t* mask, void* out, void* workspace, size_t workspace_bytes, void* stream) {
     CrossPlan p;
     if (!cross_plan(spec, mask != nullptr, &p)) return SSCATER_E_INVALID_ARG;
-    if (spec->queries == 0) return SSCATER_OK;
+    if (p.queries == 0) return SSCATER_OK;
     for (const void* x : {q, (const void*)out})
         if (!x || (uintptr_t)x % 16) return SSCATER_E_INVALID_ARG;
     for (const void* x : {k, v})
-        if ((!x && spec->keys > 0) || (uintptr_t)x % 16) return SSCATER_E_INVALID_ARG;
+        if ((!x && p.keys > 0) || (uintptr_t)x % 16) return SSCATER_E_INVALID_ARG;
     if (p.all > 0 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < p.all)) return SSCATER_E_INVALID_ARG;
-    const bool f32 = spec->dtype == SSCATER_F32, listed = mask != nullptr && spec->keys > 0;
+    const bool f32 = spec->dtype == SSCATER_F32, listed = mask != nullptr && p.keys > 0;
     const uint32_t size = f32 ? 4 : 2;
     AttendArgs a{};
-    a.rows.tokens = spec->queries; a.rows.max_new = spec->max_q; a.rows.batch = spec->batch;
+    a.rows.tokens = p.queries; a.rows.max_new = spec->max_q; a.rows.batch = spec->batch;
     a.rows.start = spec->q_start; a.rows.past = nullptr;
     a.q = q; a.k = k; a.v = v; a.out = out; a.part = (float*)workspace;
     a.q_heads = spec->q_heads; a.kv_heads = spec->kv_heads; a.group = spec->q_heads / spec->kv_heads;
@@ -175,19 +177,19 @@ int sscater_cross_attend(const sscater_cross_spec* spec, const void* q, const vo
     a.flip = spec->scale < 0.f ? f32 ? 0x80000000u : 0x80008000u : 0u;
     a.pitch_q = spec->q_stride * size;
     a.pitch_k = (uint32_t)spec->k_stride * size; a.pitch_v = (uint32_t)spec->v_stride * size;
-    a.keys = spec->keys; a.max_k = spec->max_k; a.k_start = spec->k_start;
+    a.keys = p.keys; a.max_k = spec->max_k; a.k_start = spec->k_start;
     if (listed) {
         int32_t* list = (int32_t*)((char*)workspace + p.list);
         a.list = list;
-        a.count = list + spec->keys;
+        a.count = list + p.keys;
         TokenRows keys;
-        keys.tokens = spec->keys; keys.max_new = spec->max_k; keys.batch = spec->batch; keys.start = spec->k_start;
+        keys.tokens = p.keys; keys.max_new = spec->max_k; keys.batch = spec->batch; keys.start = spec->k_start;
         keys.past = nullptr;
         const int64_t parts = std::max(1, (spec->max_k + LIST_KEYS - 1) / LIST_KEYS), groups = parts * spec->batch;
         constexpr int64_t LAUNCH = LAUNCH_GROUPS / 4;  // workgroups of 1024 threads
         for (int64_t id = 0; id < groups; id += LAUNCH)
             list_kernel<<<dim3((unsigned)std::min(LAUNCH, groups - id)), dim3(1024), 0, (hipStream_t)stream>>>(
-                mask, keys, list, list + spec->keys, (int)parts, id);
+                mask, keys, list, list + p.keys, (int)parts, id);
     }
     if (f32) {
         if (listed) launch_cross<true, Keys::LISTED>(a, p.cut, spec->head_dim, (hipStream_t)stream);

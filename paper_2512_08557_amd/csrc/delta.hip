@@ -795,7 +795,7 @@ DeltaPlan delta_plan(const sscater_delta_memory* m, const sscater_token_rows* r)
                             (k > 1 ? 5. + in * (1.5 + 1.6 * length) + 0.8 * (k - 2) : 0.);
         if (cost < best) {
             best = cost;
-            p.slots = (int64_t)r->tokens / CHUNK + m->batch;
+            p.slots = std::min((int64_t)r->tokens, (int64_t)r->max_new * m->batch) / CHUNK + m->batch;
             p.parts = (int)k;
             p.length = (int)length;
         }
@@ -907,7 +907,8 @@ int sscater_delta_update(const sscater_delta_spec* spec, const sscater_delta_mem
     const size_t need = delta_bytes(plan, memory);
     if (need > 0 && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return SSCATER_E_INVALID_ARG;
     DeltaArgs x;
-    x.rows.tokens = rows->tokens; x.rows.max_new = rows->max_new; x.rows.batch = memory->batch;
+    // (no more than the streams can have: what lies behind them needs no workspace)
+    x.rows.tokens = (int)std::min((int64_t)rows->tokens, (int64_t)rows->max_new * memory->batch); x.rows.max_new = rows->max_new; x.rows.batch = memory->batch;
     x.rows.start = rows->tokens ? rows->start : nullptr; x.rows.past = nullptr;
     x.from = initial ? initial : memory->state;
     x.state = memory->state;

@@ -43,7 +43,8 @@ def _gate(gate, dtype, index: int, shape, width: int, rows: int):
 
 
 def _call(x, block, block_norm, block_weight, block_bias, gate, activation, scale, weight, bias, eps, center, total, y,
-          stream) -> None:
+          stream):
+    """One library call; total and y (only with a weight) are made unless they are given, and returned."""
     act = GATES.get(activation, -1)
     if act < 0:
         raise ValueError(f"activation of a gate must be one of {sorted(k for k in GATES if k)}")
@@ -54,9 +55,17 @@ def _call(x, block, block_norm, block_weight, block_bias, gate, activation, scal
     rows = block.numel() // width
     ldb = _rows(block, "block" if x is not None else "x", dtype, index, shape, width)
     ldx = width if x is None else _rows(x, "x", dtype, index, shape, width)
-    lds = _rows(total, "total", dtype, index, shape, width)
-    ldy = width if y is None else _rows(y, "out", dtype, index, shape, width)
     ldg, shared = (width, 1) if gate is None else _gate(gate, dtype, index, shape, width, rows)
+    if total is None:
+        total, lds = block.new_empty(shape), width
+    else:
+        lds = _rows(total, "out" if x is None else "total", dtype, index, shape, width)
+    if y is not None:
+        ldy = _rows(y, "out", dtype, index, shape, width)
+        if y.data_ptr() == total.data_ptr() and rows:
+            raise ValueError("total and out must be two tensors")
+    else:
+        y, ldy = None if weight is None else block.new_empty(shape), width
     spec = E.NormSpec(rows, shared, width, T._KINDS[dtype], 1 if center else 0, 1 if block_norm else 0, act, eps, ldx, ldb,
                       ldg, lds, ldy)
     T._launch(lib().sscater_norm, "sscater_norm", index, stream,
@@ -65,6 +74,7 @@ def _call(x, block, block_norm, block_weight, block_bias, gate, activation, scal
               _width(block_bias, "block_bias", dtype, index, width), None if gate is None else gate.data_ptr(),
               _width(scale, "scale", dtype, index, width), _width(weight, "weight", dtype, index, width),
               _width(bias, "bias", dtype, index, width), total.data_ptr(), None if y is None else y.data_ptr())
+    return total, y
 
 
 def _tensor(t, name: str) -> None:
@@ -86,10 +96,7 @@ def norm(x, weight=None, bias=None, eps: float = 1e-6, center: bool = False, gat
     the last (one for each image of a batch, say); activation none, silu or sigmoid.
     out may be x, or a gate of its shape, and must not overlap the other operands."""
     _tensor(x, "x")
-    if out is None:
-        out = x.new_empty(x.shape)
-    _call(None, x, True, weight, bias, gate, activation, None, None, None, eps, center, out, None, stream)
-    return out
+    return _call(None, x, True, weight, bias, gate, activation, None, None, None, eps, center, out, None, stream)[0]
 
 
 def add_norm(x, block, weight=None, bias=None, *, block_weight=None, block_bias=None, gate=None,
@@ -106,12 +113,5 @@ def add_norm(x, block, weight=None, bias=None, *, block_weight=None, block_bias=
         raise ValueError("bias and out come with weight")
     if block_weight is None and block_bias is not None:
         raise ValueError("block_bias comes with block_weight")
-    if total is None:
-        total = block.new_empty(block.shape)
-    if out is None and weight is not None:
-        out = block.new_empty(block.shape)
-    if out is not None and out.data_ptr() == total.data_ptr() and block.numel():
-        raise ValueError("total and out must be two tensors")
-    _call(x, block, block_weight is not None, block_weight, block_bias, gate, activation, scale, weight, bias, eps, center,
-          total, out, stream)
-    return total, out
+    return _call(x, block, block_weight is not None, block_weight, block_bias, gate, activation, scale, weight, bias, eps,
+                 center, total, out, stream)

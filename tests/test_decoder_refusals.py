@@ -94,6 +94,21 @@ def test_cross_refuses_a_small_workspace():
     assert ssc.lib().sscater_cross_attend(None, *args, P, 1, None) == ssc.E_INVALID_ARG
 
 
+def test_rows_behind_the_last_sequence_need_no_workspace():
+    need = ctypes.c_size_t()
+    for queries, keys in ((4, 9000), (1 << 30, 9000), (4, 1 << 30), (1 << 30, 1 << 30)):
+        spec = E.CrossSpec(E.F32, 2, 8, 8, 64, queries, keys, 2, 4500, 0.1, 512, 512, 512, P, P)
+        assert ssc.lib().sscater_cross_workspace(ctypes.byref(spec), 1, ctypes.byref(need)) == ssc.OK
+        assert need.value < 64 * 4 * 8 * 66 * 4 + (9000 + 2) * 4 + 16
+    m, s = E.DeltaMemorySpec(E.F32, 2, 4, 4, 64, 64, P), E.DeltaSpec(1, 1e-6, 0.1, 256, 256, 256, 4, 4)
+    sizes = []
+    for tokens in (1000, 1 << 30):
+        rows = E.TokenRows(tokens, 500, 0, P)
+        assert ssc.lib().sscater_delta_workspace(ctypes.byref(s), ctypes.byref(m), ctypes.byref(rows), ctypes.byref(need)) == ssc.OK
+        sizes.append(need.value)
+    assert sizes[0] == sizes[1] > 0
+
+
 def test_cross_without_queries_does_nothing():
     assert _cross(queries=0, max_q=0)[0] == ssc.OK
 
