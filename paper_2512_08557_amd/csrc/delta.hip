@@ -415,7 +415,7 @@ template <bool F32, int DK, int DV, bool OUT>
 __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, const float* mats, float* parts) {
     constexpr int S = F32 ? 4 : 2;
     constexpr int NT = DK / 16, OWN = (NT + 3) / 4;    // row tiles of the state, and those of a wavefront
-    __shared__ __attribute__((aligned(16))) f4v sbuf[NT][64], zbuf[NT][64], xbuf[4][64], ubuf[4][64];
+    __shared__ __attribute__((aligned(16))) f4v sbuf[NT][64], zbuf[NT][64], xbuf[4][64], ubuf[4][64], ybuf[4][64];
     // the stretch's keys, for their transpose: rows of fp32 values, whose same columns four rows further on are 16 banks on
     constexpr int PITCH = DK + 4;
     __shared__ __attribute__((aligned(16))) float kbuf[CHUNK][PITCH];
@@ -553,7 +553,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     }
     Raw4<F32> k[NT];
     Raw1<F32> v[4];
-    f4v inv[4], fk, fb, fu[4];
+    f4v inv[4], fk, fb, fu;
     float last, keys_odd;
     uint32_t off_k = (uint32_t)(16 * w + r) * ldk + 4 * g * S, off_v[4];
 #pragma unroll
@@ -583,8 +583,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         for (int i = 0; i < 4; ++i) inv[i] = *(const f4v*)((const char*)mu + off_m + (uint32_t)min(i, w) * 1024);
     };
     auto load_s = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) fu[t] = *(const f4v*)&ms[MATS_TOKEN + TOKEN_U * CHUNK + 16 * t + 4 * g];
+        fu = *(const f4v*)&ms[MATS_TOKEN + TOKEN_U * CHUNK + 16 * w + 4 * g];
         last = ms[MATS_LAST];
     };
     // Tokens one by one, for columns with infinities or NaN in a stretch (all of them, if in its keys or gates): a product
@@ -592,7 +591,9 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     // column's rows; the state after goes to zbuf.
     auto slowly = [&](int c, uint32_t columns) __attribute__((always_inline)) {
         constexpr int R = DK / 16;
-        const int p = threadIdx.x >> 4, m = tokens(c);
+        int none = 0;
+        asm volatile("" : "+v"(none));                 // what follows is not worth registers of the loop around it
+        const int p = (threadIdx.x >> 4) + none, r = (lane & 15) + none, column = col + none, m = tokens(c);
         const bool raw = a.rate != nullptr;
         const float rate = raw ? a.rate[h] : 0.f, bias = raw ? a.bias[h] : 0.f;
         float z[R];
@@ -629,7 +630,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
                 dot = fmaf(z[j], k[j], dot);
             }
             const float u = beta_of(value_at<F32>(a.b, t * a.ldb + h), raw) *
-                            ((unit ? 0.f : value_at<F32>(a.v, t * a.ldv + h * DV + col)) - alpha * sum(dot, 0));
+                            ((unit ? 0.f : value_at<F32>(a.v, t * a.ldv + h * DV + column)) - alpha * sum(dot, 0));
 #pragma unroll
             for (int j = 0; j < R; ++j) {
                 z[j] = fmaf(k[j], u, alpha * z[j]);
@@ -697,18 +698,15 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         lds_barrier();
         const uint32_t columns = bad_columns();
         if (columns) slowly(c, columns);
-        f4v kt[OWN][4];
-#pragma unroll
-        for (int i = 0; i < OWN; ++i)
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) kt[i][t][e] = kbuf[16 * t + 4 * g + e][16 * tile(i) + r];
         f4v u[2] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t)
             if (t <= w) u[t & 1] = tile_product(inv[t], xbuf[t][lane], u[t & 1]);
-        ubuf[w][lane] = u[0] + u[1];
+        u[0] += u[1];
+        if (OUT) ubuf[w][lane] = u[0];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[0][e] *= fu[e];
+        ybuf[w][lane] = u[0];
 #pragma unroll
         for (int i = 0; i < OWN; ++i)
 #pragma unroll
@@ -719,13 +717,14 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         f4v more[OWN] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            f4v y = ubuf[t][lane];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] *= fu[t][e];
+            const f4v y = ybuf[t][lane];
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
-                if (t & 1) more[i] = tile_product(kt[i][t], y, more[i]);
-                else s[i] = tile_product(kt[i][t], y, s[i]);
+                f4v key;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) key[e] = kbuf[16 * t + 4 * g + e][16 * tile(i) + r];
+                if (t & 1) more[i] = tile_product(key, y, more[i]);
+                else s[i] = tile_product(key, y, s[i]);
             }
         }
 #pragma unroll
