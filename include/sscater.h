@@ -547,7 +547,7 @@ typedef struct {
 } sscater_delta_memory;
 
 /*   unit = 1: queries and keys are taken to unit length first, x / sqrt(sum x^2 +
- *   eps); *_stride: elements from token to token. */
+ *   eps); *_stride: elements from token to token, at most 2^24 for q, k and v. */
 typedef struct {
     int32_t unit;
     float eps, scale;
@@ -563,8 +563,10 @@ typedef struct {
  *   everything), beta = b;
  *   initial: states to begin from instead of memory->state, which is written all the
  *   same (a copy of it where a stream has no tokens), or NULL.
- * Everything is computed in fp32.  Rows behind the last stream's are left as they
- * were.  The workspace is as for attention. */
+ * Everything is computed in fp32, tokens one by one or in stretches of 64, which
+ * differ in their last bits; a stream's stretches are also what its tokens depend on:
+ * none on later ones, whatever those hold.  Rows behind the last stream's are left as
+ * they were.  The workspace is as for attention. */
 int sscater_delta_workspace(const sscater_delta_spec* spec, const sscater_delta_memory* memory,
                             const sscater_token_rows* rows, size_t* bytes);
 int sscater_delta_update(const sscater_delta_spec* spec, const sscater_delta_memory* memory,

@@ -40,7 +40,7 @@ void launch_attend(AttendArgs a, const AttendCut& cut, hipStream_t s) {
         if (cut.wm == 2) attend_kernel<F32, D, 2, Keys::CACHE><<<grid, block, 0, s>>>(a);
         if (cut.wm == 4) attend_kernel<F32, D, 4, Keys::CACHE><<<grid, block, 0, s>>>(a);
     }
-    if (cut.splits > 1) {                              // at most some hundred thousand rows: see attend_cut
+    if (cut.splits > 1) {                              // at most some hundred thousand rows: see cut_keys
         const int64_t rows = (int64_t)a.rows.tokens * a.q_heads;
         join_kernel<F32, D, true><<<dim3((unsigned)((rows + 3) / 4)), block, 0, s>>>(a.part, a.out, rows, cut.splits,
                                                                                      a.q_heads, rows_end(a.rows));
