@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256) void delta_token_kernel(DeltaArgs a) {
 constexpr int CHUNK = 64;
 // What is kept of a stretch for each head: the ten lower tiles of T and of P, each as a wavefront reads it as a first
 // operand (lane 16 g + r: row r, columns 4 g .. 4 g + 3), four factors of every token, e^G_63 and whether something is
-// infinite or NaN.
+// infinite, NaN or, in T, so large that U might be.
 constexpr int MATS_P = 10 * 256, MATS_TOKEN = 20 * 256, MATS_LAST = MATS_TOKEN + 4 * CHUNK, MATS = MATS_LAST + 16;
 enum { TOKEN_K, TOKEN_U, TOKEN_Q, TOKEN_BETA };
 
@@ -221,6 +221,10 @@ __device__ __forceinline__ f4v tile_product(const f4v x, const f4v y, f4v c) {
 __device__ __forceinline__ int slot_of(int first, int b) { return first / CHUNK + b; }
 
 __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
+// Of 2^e or more, infinite or NaN.
+__device__ __forceinline__ bool beyond(float v, int e) { return (__float_as_uint(v) & 0x7F800000u) >= (uint32_t)(127 + e) << 23; }
+// T and X below these make 64 sums that are finite.
+constexpr int T_LIMIT = 20, X_LIMIT = 100;
 
 template <bool F32, int DK>
 __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
@@ -386,6 +390,14 @@ __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
             column[i] = -y;
             keep(i, column[i]);
         }
+    bool large = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i >= w)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) large |= beyond(column[i][e], T_LIMIT);
+    large = __ballot(large) != 0;
+    if (lane == 0 && large) bad[w] = 1;
     __syncthreads();
     for (int t = w; t < 10; t += 4) {
         *(f4v*)&out[t * 256 + lane * 4] = operand(shared, t);
@@ -586,8 +598,8 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         fu = *(const f4v*)&ms[MATS_TOKEN + TOKEN_U * CHUNK + 16 * w + 4 * g];
         last = ms[MATS_LAST];
     };
-    // Tokens one by one, for columns with infinities or NaN in a stretch (all of them, if in its keys or gates): a product
-    // with a triangle's zeros would carry them to the tokens before.  Thread 16 p + column has the p-th sixteenth of a
+    // Tokens one by one, for columns with infinities or NaN in a stretch, or values that might become some (all of them, if
+    // in its keys or gates): a product with a triangle's zeros would carry them to the tokens before.  Thread 16 p + column has the p-th sixteenth of a
     // column's rows; the state after goes to zbuf.
     auto slowly = [&](int c, uint32_t columns) __attribute__((always_inline)) {
         constexpr int R = DK / 16;
@@ -684,7 +696,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         for (int e = 0; e < 4; ++e) {
             const float value = 16 * w + 4 * g + e < m && !unit ? v[e].get() : 0.f;
             x[0][e] = fmaf(fb[e], value, -fk[e] * (x[0][e] + x[1][e]));
-            odd |= !finite(value);
+            odd |= beyond(x[0][e], X_LIMIT);
         }
         xbuf[w][lane] = x[0];
         const uint64_t lanes = __ballot(odd);

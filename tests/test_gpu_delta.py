@@ -261,6 +261,32 @@ def test_no_token_sees_a_later_one(at, value, where, kind):
         assert not bool(torch.isfinite(out[s0][at:]).any())
 
 
+@pytest.mark.parametrize("what", ["no direction", "large key", "large correction"])
+@pytest.mark.parametrize("at", [70, 93, 701])
+def test_no_token_sees_what_overflows_later(at, what):
+    """Finite tokens whose products are not: a key of zeros taken to unit length without
+    an eps, one whose square passes the range, a value whose product with its key does.
+    (Without the eps of the 64-bit results a key of length 4 or more is off by 2^-25.)"""
+    n = 150 if at < 150 else 1500
+    unit = what == "no direction"
+    c = Case(16, [n, 90], 2, 1, 64, 32, "f32", raw=False, unit=unit)
+    (_, s0, _, _, ref, tol), (_, s1, _, _, ref1, tol1) = c.sequences()
+    assert not unit or float(c.k.norm(dim=-1).min()) >= 4
+    if unit:
+        c.k[at] = 0
+    elif what == "large key":
+        c.k[at] = 1e25
+    else:
+        c.k[at] *= 400
+        c.v[at, 1, 3] = 1e38
+    out = c.call(eps=0.0, start=c.start, max_new=n)
+    bound(out[s0][:at], ref[:at], tol[:at], "before")
+    bound(out[s1], ref1, tol1, "the other stream")
+    if what == "large correction":
+        keep = [i for i in range(32) if i != 3]
+        assert bool(torch.isfinite(out[s0][:, 1, keep]).all()) and bool(torch.isfinite(out[s0][:, 0]).all())
+
+
 @pytest.mark.parametrize("n", [1, 130])
 def test_a_captured_update_replays(n):
     rng = np.random.default_rng(12)
