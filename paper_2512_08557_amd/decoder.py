@@ -23,7 +23,7 @@ from typing import Dict, Optional
 from .cross import cross_attend
 from .delta import DeltaMemory
 from .norms import add_norm, norm
-from .tokens import linear
+from .tokens import _require, _row_stride, _want_gradient, linear
 
 NAMES = ("norm", "memory", "memory_gate", "memory_norm", "memory_out", "cross_norm", "q", "kv", "cross_out", "ffn_norm",
          "up", "down", "out_norm")
@@ -51,7 +51,8 @@ class QueryDecoder:
         missing = [n for n in NAMES + FLOATS if n not in weights]
         if missing:
             raise ValueError(f"weights without {missing}")
-        self.weights, kind = dict(weights), weights["q"].dtype
+        self.weights = {n: weights[n] for n in NAMES + FLOATS + OPTIONAL if weights.get(n) is not None}
+        kind, index = weights["q"].dtype, weights["q"].get_device()
         dtype = {torch.float32: "f32", torch.bfloat16: "bf16"}.get(kind)
         if dtype is None:
             raise ValueError(f"weights must be float32 or bfloat16, not {kind}")
@@ -74,6 +75,11 @@ class QueryDecoder:
         for name in NAMES + FLOATS + OPTIONAL:
             if weights.get(name) is not None and tuple(weights[name].shape) != shapes.get(name, (width,)):
                 raise ValueError(f"{name} must be {shapes.get(name, (width,))}, not {tuple(weights[name].shape)}")
+        for name, t in self.weights.items():
+            _require(t, name, torch.float32 if name in FLOATS else kind, index)
+            if t.dim() == 1 and not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+            _row_stride(t, name, t.shape[-1])
         if self.kv_heads < 1 or self.q_heads % self.kv_heads or self.head_dim not in (32, 64, 128):
             raise ValueError("q_heads a multiple of kv_heads, head_dim 32, 64 or 128")
 
@@ -85,6 +91,8 @@ class QueryDecoder:
         w, m, eps, width = self.weights, self.memory, self.eps, x.shape[-1]
         shape, n = (self.batch, self.queries, width), self.batch * self.queries
         # before the memory is changed, which a later refusal would leave so
+        if x.requires_grad or any(t.requires_grad for t in w.values()):
+            _want_gradient()
         if x.shape != shape:
             raise ValueError(f"x must be {shape}, not {tuple(x.shape)}")
         if cells.dim() != 3 or cells.shape[0] != self.batch or cells.shape[2] != w["kv"].shape[1]:

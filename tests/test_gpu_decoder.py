@@ -113,6 +113,26 @@ def test_a_refused_stride_leaves_the_memory():
         assert torch.equal(dec.memory.state, state)
 
 
+def test_weights_that_a_later_call_would_refuse():
+    """A weight behind the memory's: refused when the decoder is made or before the memory is changed."""
+    w = make_weights(np.random.default_rng(6), torch.float32)
+    args = (QUERIES, MH, DK, DV, QH, KV, DIM)
+    wide = torch.ones(C, 2, device="cuda")
+    for bad, name in (({"out_norm": wide[:, 0]}, "out_norm"), ({"down": w["down"].t().contiguous().t()}, "down"),
+                      ({"up": w["up"].cpu()}, "up"), ({"rate": w["rate"].double()}, "rate")):
+        with pytest.raises(ValueError, match=name):
+            QueryDecoder(dict(w, **bad), *args, qk_heads=QK)
+    dec = QueryDecoder(w, *args, qk_heads=QK)
+    x, cells = torch.randn(1, QUERIES, C, device="cuda"), torch.randn(1, 70, CELLS, device="cuda")
+    w["down"].requires_grad_(True)
+    with pytest.raises(ValueError, match="gradient"):
+        dec.step(x, cells)
+    assert not bool(dec.memory.state.any())
+    with torch.no_grad():
+        dec.step(x, cells)
+    assert bool(dec.memory.state.any())
+
+
 def test_captured_strides_replay():
     """A whole stride in a graph: replays go on from stride to stride as eager calls do."""
     rng = np.random.default_rng(4)
