@@ -474,7 +474,8 @@ int sscater_tokens_advance(const sscater_token_cache* cache, const sscater_token
  *   P(u) = (u - c) / sqrt(mean((u - c)^2) + eps) * block_weight + block_bias,
  * c the mean of the row (center = 1) or zero; N the same with weight and bias.
  * sum and y are formed from fp32 values and rounded once each (y from the sum
- * before its rounding).
+ * before its rounding); squares are summed in fp32, which they overflow from
+ * values of 2^64 / sqrt(width) on (the quotient is zero there).
  *   rows >= 0, width >= 1 (rows <= 2^36, width <= 2^30, rows * width <= 2^40);
  *   block_norm = 0: block itself in P's place; activation (of the gate): NONE,
  *   SILU or SIGMOID; gate_rows: consecutive rows that share a row of the gate
@@ -547,7 +548,7 @@ typedef struct {
 } sscater_delta_memory;
 
 /*   unit = 1: queries and keys are taken to unit length first, x / sqrt(sum x^2 +
- *   eps); *_stride: elements from token to token, at most 2^24 for q, k and v. */
+ *   eps), the squares summed in fp32 as in the norms; *_stride: elements from token to token, at most 2^24 for q, k and v. */
 typedef struct {
     int32_t unit;
     float eps, scale;

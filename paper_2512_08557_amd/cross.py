@@ -3,6 +3,7 @@ only).  It forms no gradients: where one would be wanted it refuses the call."""
 from __future__ import annotations
 
 import ctypes
+from functools import lru_cache
 from typing import Optional
 
 from . import engine as E
@@ -37,6 +38,17 @@ def _heads(t, name: str, dtype, index: int, dims: int) -> int:
     if t.requires_grad:
         T._want_gradient()
     return ld
+
+
+def _describe(masked: int, *fields):
+    """A call's description, and the bytes of its workspace."""
+    spec, need = E.CrossSpec(*fields), ctypes.c_size_t()
+    _check(lib().sscater_cross_workspace(spec, masked, need), "sscater_cross_workspace")
+    return spec, need.value
+
+
+# of sizes alone, without addresses (2.6 us to make, 0.2 to find)
+_described = lru_cache(256)(_describe)
 
 
 def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional[int] = None,
@@ -103,13 +115,11 @@ def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional
         raise ValueError("out must be on a 16-byte boundary")
     if queries == 0:
         return out
-    spec = E.CrossSpec(kind, batch, heads, k.shape[-2], dim, queries, keys, max_q, max_k,
-                       dim ** -0.5 if scale is None else scale, ldq, ldk, ldv, *at)
-    need, work = ctypes.c_size_t(), None
-    _check(lib().sscater_cross_workspace(spec, 0 if mask is None else 1, need), "sscater_cross_workspace")
-    if need.value:
-        work = q.new_empty(need.value, dtype=T.torch.uint8)
+    spec, need = (_described if q_start is None else _describe)(
+        0 if mask is None else 1, kind, batch, heads, k.shape[-2], dim, queries, keys, max_q, max_k,
+        dim ** -0.5 if scale is None else scale, ldq, ldk, ldv, *at)
+    work = q.new_empty(need, dtype=T.torch.uint8) if need else None
     T._launch(lib().sscater_cross_attend, "sscater_cross_attend", index, stream, (q, k, v, mask, q_start, k_start, out, work),
               spec, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if mask is None else mask.data_ptr(), out.data_ptr(),
-              None if work is None else work.data_ptr(), need.value)
+              None if work is None else work.data_ptr(), need)
     return out
