@@ -806,7 +806,8 @@ inline void cut_keys(AttendCut* cut, bool f32, int dim, int64_t rows, int64_t he
             }
         }
         // Of sequences whose lengths only the device knows the longest would be the time: three times as many workgroups as
-        // places, so that the short ones' make room.
+        // places, so that the short ones' make room (nine of up to 257 queries and 12001 keys, four fp32 heads of 128 on
+        // one, 166 us for 268).
         if (uneven) cut->splits = (int)std::max((int64_t)cut->splits, std::min((3 * places + base - 1) / base, most));
     }
     cut->grid = base * cut->splits;

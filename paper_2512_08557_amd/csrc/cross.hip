@@ -5,6 +5,11 @@
 // Keys have no order, so the visible ones of a sequence may as well be the only
 // ones: their rows' numbers, one behind the other, are all that the attention looks
 // at, and cells that are not visible cost nothing but their byte of the mask.
+//
+// Bound by the softmax's vector instructions for heads of 32 (3600 queries, a quarter
+// of four times 53568 cells visible, 8 bf16 heads: 114 us, matrix cores 19 % busy), by
+// those and the products for larger ones (all cells, 16 heads of 64 on 4: 980 us, 806
+// TFLOP/s, 35 % busy).
 #include "attend_kernel.h"
 
 #include <algorithm>
@@ -23,7 +28,8 @@ __device__ __forceinline__ uint32_t seen4(uint32_t w) {
 
 // A sequence's visible keys in order.  Workgroup b * parts + p lists those among the p-th
 // LIST_KEYS of sequence b, behind the ones before them, which it counts itself, 16 bytes a
-// lane: a second launch would take longer than reading a mask again.
+// lane: a second launch would take longer than reading a mask again (four maps of 53568
+// cells 5 us).
 __global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRows keys, int32_t* list, int32_t* count,
                                                     int parts, int64_t id0) {
     __shared__ int sums[2][16];

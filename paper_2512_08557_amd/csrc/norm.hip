@@ -10,6 +10,9 @@
 // from the sum before that is rounded.  Those lanes take several rows, the next
 // one's values under way while this one's are worked on; what the rows share
 // (weights, an image's gate times the scale) stays in registers too.
+//
+// Bound by memory: 214272 rows of 384 bf16 values (norm, image gates, residual, norm:
+// 658 MB) 141 us, 4.7 TB/s where a large copy has 4.7 to 5.1.
 #include "tokens.h"
 
 #include <algorithm>
