@@ -143,6 +143,20 @@ def test_strides_and_the_axis_that_may_be_missing(queries, kind):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [32, 128])
+@pytest.mark.parametrize("queries,masked", [(1, False), (2, True), (50, False), (140, True), (130, False)])
+def test_rows_far_apart(queries, masked, dim, kind):
+    """The largest stride, 2^24 elements: a tile's rows lie up to 2^32 bytes apart, and the last ones further on."""
+    note(f"[gpu-test] cross {queries} queries, rows 2^24 elements apart, {dim} {kind}")
+    rng = np.random.default_rng(queries)
+    rows = torch.empty((140, 1 << 24), dtype=KIND[kind], device="cuda")
+    rows[:, -6 * dim:] = normal(rng, (140, 6 * dim), KIND[kind])
+    q, k, v = (rows[:, (i - 6) * dim:(i - 4) * dim or None].unflatten(1, (2, dim)) for i in (0, 2, 4))
+    mask = torch.from_numpy(rng.random(140) < 0.6).cuda() if masked else None
+    close(ssc.cross_attend(q[:queries], k, v, mask), *reference(q[:queries], k, v, mask, dim ** -0.5, kind), "far apart")
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("queries", [1, 40, 200])
 def test_scales_and_large_scores(queries, kind):
     rng = np.random.default_rng(queries)

@@ -189,6 +189,41 @@ def test_parts_of_a_stream_are_the_stream():
     assert bool(((c.memory.state[0].double().cpu() - S).norm(dim=1) <= err + 2 * U * S.norm(dim=1)).all())
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,dk,dv", [([140], 64, 64), ([2, 138], 128, 32), ([5, 4], 32, 64)])
+def test_tokens_far_apart(counts, dk, dv, kind):
+    """The largest stride, 2^24 elements: a stretch's tokens lie up to 2^32 bytes apart, and the last ones further on."""
+    c = Case(sum(counts), counts, 2, 1, dk, dv, kind)
+    rows, at = torch.empty((sum(counts), 1 << 24), dtype=KIND[kind], device="cuda"), 1 << 24
+    for name in "qkvab":
+        t = getattr(c, name)
+        width = t[0].numel()
+        at -= width
+        view = rows[:, at:at + width]
+        view.copy_(t.reshape(len(t), -1))
+        setattr(c, name, view.unflatten(1, t.shape[1:]) if t.dim() == 3 else view)
+    c.check(start=c.start, max_new=max(counts))
+
+
+def test_more_than_4_gib_of_states():
+    """70001 streams of 128 x 128, a token each: the first, the last and one between."""
+    n = 70001
+    rng = np.random.default_rng(8)
+    q, k, v = (normal(rng, (n, 1, 128), torch.float32) for _ in range(3))
+    a, b = -normal(rng, (n, 1), torch.float32).abs(), torch.sigmoid(normal(rng, (n, 1), torch.float32))
+    state = torch.randn((n, 1, 128, 128), device="cuda")
+    pick = [0, 33333, n - 1]
+    before = state[pick].double().cpu()
+    m = ssc.DeltaMemory(n, 1, 128, 128, state=state)
+    out = m.update(q, k, v, a, b)
+    q, k, v, a, b = (t[pick].double().cpu()[:, None] for t in (q, k, v, a, b))
+    q, k = (x / torch.sqrt((x * x).sum(-1, keepdim=True) + 1e-6) for x in (q, k))
+    for i, s in enumerate(pick):
+        S, err, ref, tol = recurrence(before[i], q[i], k[i], v[i], torch.exp(a[i]), b[i], 128 ** -0.5, "f32")
+        bound(out[s:s + 1], ref, tol, f"stream {s}")
+        assert bool(((state[s].double().cpu() - S).norm(dim=1) <= err + 2 * U * S.norm(dim=1)).all())
+
+
 @pytest.mark.parametrize("n", [1, 100, 1500])
 def test_initial_states(n):
     """Beginning from other states leaves those as they were and writes the memory's,

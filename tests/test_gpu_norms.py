@@ -154,6 +154,32 @@ def test_strides_alignment_and_what_is_not_written(width, pad, offset, kind):
         assert torch.equal(flat[mask], was[mask])
 
 
+@pytest.mark.parametrize("width", [40, 9001])
+def test_rows_far_apart(width):
+    """Rows 2^25 values apart, all within one tensor: the last ones begin behind 2^32 bytes and values."""
+    rng = np.random.default_rng(width)
+    rows = torch.empty((140, 1 << 25), dtype=torch.bfloat16, device="cuda")
+    x, block, gate, total, out = (rows[:, i * width:(i + 1) * width] for i in range(5))
+    for t in (x, block, gate):
+        t.copy_(normal(rng, (140, width), torch.bfloat16))
+    w = normal(rng, (width,), torch.bfloat16, 0.2, 1)
+    ssc.add_norm(x, block, w, gate=gate, total=total, out=out)
+    ref = reference(x, block, w, None, None, None, gate, None, None, 1e-6, False, "bf16")
+    close(total, *ref[0], "total")
+    close(out, *ref[1], "out")
+
+
+def test_more_than_2_to_32_values():
+    rows, width = (1 << 32) // 1000 + 77, 1000
+    x = torch.randn((rows, width), dtype=torch.bfloat16, device="cuda")
+    w = normal(np.random.default_rng(1), (width,), torch.bfloat16, 0.2, 1)
+    total, out = ssc.add_norm(x, x, w)
+    for s in (slice(0, 50), slice(rows // 2, rows // 2 + 50), slice(rows - 50, rows)):
+        ref = reference(x[s], x[s], w, None, None, None, None, None, None, 1e-6, False, "bf16")
+        close(total[s], *ref[0], "total")
+        close(out[s], *ref[1], "out")
+
+
 @pytest.mark.parametrize("width", [64, 300, 3000, 20000])
 def test_in_place(width):
     """The sum in the residual's or the block's place, the norm in the other's; a gate's."""
