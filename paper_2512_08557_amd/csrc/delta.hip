@@ -291,8 +291,9 @@ __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
         kk += __shfl_xor(kk, 32);
         qq += __shfl_xor(qq, 32);
         if (g == 0) {
-            unit_k[tk] = a.unit ? 1.f / sqrtf(kk + a.eps) : 1.f;
-            unit_q[tq] = (a.unit ? 1.f / sqrtf(qq + a.eps) : 1.f) * a.scale;
+            // (behind the last token zero, whatever eps)
+            unit_k[tk] = tk >= m ? 0.f : a.unit ? 1.f / sqrtf(kk + a.eps) : 1.f;
+            unit_q[tq] = tq >= m ? 0.f : (a.unit ? 1.f / sqrtf(qq + a.eps) : 1.f) * a.scale;
         }
     }
     if (w == 0) {
@@ -438,9 +439,12 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     constexpr int S = F32 ? 4 : 2;
     constexpr int NT = DK / 16, OWN = (NT + 3) / 4;    // row tiles of the state, and those of a wavefront
     __shared__ __attribute__((aligned(16))) f4v sbuf[NT][64], zbuf[NT][64], xbuf[4][64], ubuf[4][64], ybuf[4][64];
-    // the stretch's keys, for their transpose: rows of fp32 values, whose same columns four rows further on are 16 banks on
-    constexpr int PITCH = DK + 4;
-    __shared__ __attribute__((aligned(16))) float kbuf[CHUNK][PITCH];
+    // bf16 keys and queries: the state and Y as three bf16 planes each, second operands of 32 rows (two tiles)
+    __shared__ __attribute__((aligned(16))) uint4 splanes[F32 ? 1 : NT / 2 * 3][64], yplanes[F32 ? 1 : 2 * 3][64];
+    // the stretch's keys, for their transpose: rows of fp32 values, whose same columns four rows further on are 16 banks
+    // on, or of bf16 ones
+    constexpr int PITCH = DK * S + 16;
+    __shared__ __attribute__((aligned(16))) char kbuf[CHUNK * PITCH];
     __shared__ float part[2][16][16];
     __shared__ uint32_t bad[4];
     // the columns of a head follow one another on one XCD (workgroup id mod 8), whose L2 then has its keys and matrices
@@ -476,11 +480,41 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         if constexpr (F32) ((float*)a.out)[to] = v;
         else ((uint16_t*)a.out)[to] = (uint16_t)bf16_pair(v, v);
     };
+    // a tile as planes, behind or before its neighbour's rows
+    auto cut = [&](const f4v v, uint4 (*to)[64], int tile) __attribute__((always_inline)) {
+        typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+        uint32_t x[3], y[3];
+        cut_pair(__float_as_uint(v[0]), __float_as_uint(v[1]), x[0], x[1], x[2]);
+        cut_pair(__float_as_uint(v[2]), __float_as_uint(v[3]), y[0], y[1], y[2]);
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            *(u2v*)((char*)&to[tile / 2 * 3 + i][lane] + tile % 2 * 8) = u2v{x[i], y[i]};
+    };
+    // rows of keys or queries times the state
+    auto rows_times_state = [&](const Raw4<F32> (&x)[NT]) __attribute__((always_inline)) {
+        if constexpr (F32) {
+            // two sums: an instruction need not wait for the one before it
+            f4v c[2] = {};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) c[t & 1] = tile_product(x[t].get(), sbuf[t][lane], c[t & 1]);
+            return c[0] + c[1];
+        } else {
+            f4v c[3] = {};
+#pragma unroll
+            for (int t = 0; t < NT; t += 2) {
+                const uint4 v = make_uint4(x[t].w[0], x[t].w[1], x[t + 1].w[0], x[t + 1].w[1]);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) c[i] = mfma_bf16(v, splanes[t / 2 * 3 + i][lane], c[i]);
+            }
+            return c[0] + (c[1] + c[2]);
+        }
+    };
     // the same from all of a workgroup's wavefronts
     auto bad_columns = [&]() __attribute__((always_inline)) {
         return __builtin_amdgcn_readfirstlane((bad[0] | bad[1] | bad[2] | bad[3]) & 0xFFFFu);
     };
     const int sums = a.unit ? 4 : 2;                   // of a token taken by itself
+    constexpr int HAND = F32 ? 0 : 1;                  // meeting before those, for the state in fp32
 
     if (OUT && wave >= 4) {
         Raw4<F32> q[NT];
@@ -517,15 +551,10 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             lds_barrier();
             const uint32_t columns = bad_columns();
             if (columns)
-                for (int i = m * sums; i > 0; --i) lds_barrier();
-            f4v o[2] = {};
+                for (int i = m * sums + HAND; i > 0; --i) lds_barrier();
+            f4v o[2] = {rows_times_state(q), {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-            for (int t = 0; t < NT; ++t) o[t & 1] = tile_product(q[t].get(), sbuf[t][lane], o[t & 1]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                o[0][e] = (o[0][e] + o[1][e]) * fq[e];
-                o[1][e] = 0.f;
-            }
+            for (int e = 0; e < 4; ++e) o[0][e] *= fq[e];
             if (c + 1 < chunks) {
                 at += step_q;
                 mx += step_m;
@@ -553,6 +582,11 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     }
 
     f4v s[OWN];
+    // for the products with it; and as it is, which a slow stretch and the parts before take
+    auto give = [&](int t, const f4v v) __attribute__((always_inline)) {
+        if constexpr (F32) sbuf[t][lane] = v;
+        else cut(v, splanes, t);
+    };
     auto tile = [&](int o) __attribute__((always_inline)) { return NT < 4 ? min(w, NT - 1) : w + 4 * o; };
     const bool own = NT >= 4 || w < NT;
     auto state_at = [&](int o, int e) __attribute__((always_inline)) {
@@ -572,6 +606,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             for (int e = 0; e < 4; ++e) s[o][e] = unit && 16 * tile(o) + 4 * g + e == col ? 1.f : 0.f;
         }
         if (own) sbuf[tile(o)][lane] = s[o];
+        if (!F32 && own) cut(s[o], splanes, tile(o));
     }
     Raw4<F32> k[NT];
     Raw1<F32> v[4];
@@ -619,6 +654,12 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         const bool raw = a.rate != nullptr;
         const float rate = raw ? a.rate[h] : 0.f, bias = raw ? a.bias[h] : 0.f;
         float z[R];
+        if constexpr (!F32) {
+#pragma unroll
+            for (int o = 0; o < OWN; ++o)
+                if (own) sbuf[tile(o)][lane] = s[o];
+            lds_barrier();
+        }
         auto place = [&](f4v (&buf)[NT][64], int i) __attribute__((always_inline)) {
             const int row = p * R + i;
             return &((float*)&buf[row / 16][16 * (row % 16 / 4) + r])[row % 4];
@@ -686,6 +727,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             for (int o = 0; o < OWN; ++o) {
                 s[o] = y[o];
                 if (own) sbuf[tile(o)][lane] = s[o];
+                if (!F32 && own) cut(s[o], splanes, tile(o));
             }
             lds_barrier();
         }
@@ -693,22 +735,17 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
 #pragma unroll 1
     for (int c = c0; c < chunks; ++c) {
         const int m = tokens(c), next = min(c + 1, chunks - 1);
-        // two sums: an instruction need not wait for the one before it
-        f4v x[2] = {};
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const f4v key = k[t].get();
-            *(f4v*)&kbuf[16 * w + r][16 * t + 4 * g] = key;
-            x[t & 1] = tile_product(key, sbuf[t][lane], x[t & 1]);
-        }
+        for (int t = 0; t < NT; ++t) __builtin_memcpy(kbuf + (16 * w + r) * PITCH + (16 * t + 4 * g) * S, k[t].w, sizeof k[t].w);
+        f4v x = rows_times_state(k);
         bool odd = keys_odd != 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float value = 16 * w + 4 * g + e < m && !unit ? v[e].get() : 0.f;
-            x[0][e] = fmaf(fb[e], value, -fk[e] * (x[0][e] + x[1][e]));
-            odd |= beyond(x[0][e], X_LIMIT);
+            x[e] = fmaf(fb[e], value, -fk[e] * x[e]);
+            odd |= beyond(x[e], X_LIMIT);
         }
-        xbuf[w][lane] = x[0];
+        xbuf[w][lane] = x;
         const uint64_t lanes = __ballot(odd);
         if (lane == 0) bad[w] = (uint32_t)(lanes | lanes >> 32) | (uint32_t)(lanes >> 16 | lanes >> 48);
         if (c + 1 < chunks) {
@@ -728,7 +765,8 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         if (OUT) ubuf[w][lane] = u[0];
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[0][e] *= fu[e];
-        ybuf[w][lane] = u[0];
+        if constexpr (F32) ybuf[w][lane] = u[0];
+        else cut(u[0], yplanes, w);
 #pragma unroll
         for (int i = 0; i < OWN; ++i)
 #pragma unroll
@@ -736,24 +774,44 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         if (c + 1 < chunks) mu += step_m;
         load_u();
         lds_barrier();
-        f4v more[OWN] = {};
+        f4v more[OWN] = {}, least[OWN] = {};
+        if constexpr (F32) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const f4v y = ybuf[t][lane];
+            for (int t = 0; t < 4; ++t) {
+                const f4v y = ybuf[t][lane];
 #pragma unroll
-            for (int i = 0; i < OWN; ++i) {
-                f4v key;
+                for (int i = 0; i < OWN; ++i) {
+                    f4v key;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) key[e] = kbuf[16 * t + 4 * g + e][16 * tile(i) + r];
-                if (t & 1) more[i] = tile_product(key, y, more[i]);
-                else s[i] = tile_product(key, y, s[i]);
+                    for (int e = 0; e < 4; ++e) key[e] = *(const float*)(kbuf + (16 * t + 4 * g + e) * PITCH + (16 * tile(i) + r) * S);
+                    if (t & 1) more[i] = tile_product(key, y, more[i]);
+                    else s[i] = tile_product(key, y, s[i]);
+                }
             }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; t += 2)
+#pragma unroll
+                for (int i = 0; i < OWN; ++i) {
+                    // (a transposing read: 16 lanes take 4 rows of 16 keys' values, each lane a column of them)
+                    typedef short s4v __attribute__((ext_vector_type(4)));
+                    typedef __attribute__((address_space(3))) s4v lds_s4v;
+                    const lds_char* at = (const lds_char*)kbuf + (16 * t + 4 * g + (r >> 2)) * PITCH + (16 * tile(i) + 4 * (r & 3)) * S;
+                    const s4v k0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)at);
+                    const s4v k1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + 16 * PITCH));
+                    uint4 key;
+                    __builtin_memcpy(&key, &k0, 8);
+                    __builtin_memcpy((char*)&key + 8, &k1, 8);
+                    s[i] = mfma_bf16(key, yplanes[t / 2 * 3][lane], s[i]);
+                    more[i] = mfma_bf16(key, yplanes[t / 2 * 3 + 1][lane], more[i]);
+                    least[i] = mfma_bf16(key, yplanes[t / 2 * 3 + 2][lane], least[i]);
+                }
         }
 #pragma unroll
         for (int i = 0; i < OWN; ++i) {
-            s[i] += more[i];
+            s[i] += F32 ? more[i] : more[i] + least[i];
             if (columns >> r & 1) s[i] = zbuf[tile(i)][lane];
-            if (own) sbuf[tile(i)][lane] = s[i];
+            if (own) give(tile(i), s[i]);
         }
         if (c + 1 < chunks) ms += step_m;
         load_s();
