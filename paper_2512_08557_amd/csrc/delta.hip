@@ -439,12 +439,15 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     constexpr int S = F32 ? 4 : 2;
     constexpr int NT = DK / 16, OWN = (NT + 3) / 4;    // row tiles of the state, and those of a wavefront
     __shared__ __attribute__((aligned(16))) f4v sbuf[NT][64], zbuf[NT][64], xbuf[4][64], ubuf[4][64], ybuf[4][64];
-    // bf16 keys and queries: the state and Y as three bf16 planes each, second operands of 32 rows (two tiles)
-    __shared__ __attribute__((aligned(16))) uint4 splanes[F32 ? 1 : NT / 2 * 3][64], yplanes[F32 ? 1 : 2 * 3][64];
-    // the stretch's keys, for their transpose: rows of fp32 values, whose same columns four rows further on are 16 banks
-    // on, or of bf16 ones
-    constexpr int PITCH = DK * S + 16;
-    __shared__ __attribute__((aligned(16))) char kbuf[CHUNK * PITCH];
+    // PL: the state and Y as three bf16 planes each, second operands of 32 rows (two tiles), and as first ones the keys, one
+    // plane if they are bf16 and three if not.  Without outputs fp32 keys stay fp32: nobody is there to cut them.
+    constexpr bool PL = !F32 || OUT;
+    constexpr int KP = F32 ? 3 : 1;
+    __shared__ __attribute__((aligned(16))) uint4 splanes[PL ? NT / 2 * 3 : 1][64], yplanes[PL ? 2 * 3 : 1][64];
+    // The stretch's keys and, from the outputs' wavefronts, the next one's.  PL: 32 columns' 16-byte pieces are four of
+    // columns 4 g .. 4 g + 3 and of 4 g + 16 .. 4 g + 19, as the products take them.
+    constexpr int PITCH = DK * (PL ? 2 : 4) + 16, PLANE = CHUNK * PITCH, KEYS = (PL ? KP : 1) * PLANE;
+    __shared__ __attribute__((aligned(16))) char kbuf[(OUT ? 2 : 1) * KEYS];
     __shared__ float part[2][16][16];
     __shared__ uint32_t bad[4];
     // the columns of a head follow one another on one XCD (workgroup id mod 8), whose L2 then has its keys and matrices
@@ -480,41 +483,112 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         if constexpr (F32) ((float*)a.out)[to] = v;
         else ((uint16_t*)a.out)[to] = (uint16_t)bf16_pair(v, v);
     };
+    typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+    auto planes_of = [&](const f4v v, u2v (&x)[3]) __attribute__((always_inline)) {
+        uint32_t a[3], b[3];
+        cut_pair(__float_as_uint(v[0]), __float_as_uint(v[1]), a[0], a[1], a[2]);
+        cut_pair(__float_as_uint(v[2]), __float_as_uint(v[3]), b[0], b[1], b[2]);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) x[i] = u2v{a[i], b[i]};
+    };
     // a tile as planes, behind or before its neighbour's rows
     auto cut = [&](const f4v v, uint4 (*to)[64], int tile) __attribute__((always_inline)) {
-        typedef uint32_t u2v __attribute__((ext_vector_type(2)));
-        uint32_t x[3], y[3];
-        cut_pair(__float_as_uint(v[0]), __float_as_uint(v[1]), x[0], x[1], x[2]);
-        cut_pair(__float_as_uint(v[2]), __float_as_uint(v[3]), y[0], y[1], y[2]);
+        u2v x[3];
+        planes_of(v, x);
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-            *(u2v*)((char*)&to[tile / 2 * 3 + i][lane] + tile % 2 * 8) = u2v{x[i], y[i]};
+        for (int i = 0; i < 3; ++i) *(u2v*)((char*)&to[tile / 2 * 3 + i][lane] + tile % 2 * 8) = x[i];
     };
-    // rows of keys or queries times the state
-    auto rows_times_state = [&](const Raw4<F32> (&x)[NT]) __attribute__((always_inline)) {
-        if constexpr (F32) {
+    // 32 rows' product: of nine of planes the six that fp32 holds
+    auto plane_products = [&](const uint4 (&x)[KP], const uint4 (*y)[64], f4v (&c)[3]) __attribute__((always_inline)) {
+        const uint4 y0 = y[0][lane], y1 = y[1][lane], y2 = y[2][lane];
+        c[0] = mfma_bf16(x[0], y0, c[0]);
+        c[1] = mfma_bf16(x[0], y1, c[1]);
+        c[2] = mfma_bf16(x[0], y2, c[2]);
+        if constexpr (KP == 3) {
+            c[1] = mfma_bf16(x[1], y0, c[1]);
+            c[2] = mfma_bf16(x[1], y1, c[2]);
+            c[2] = mfma_bf16(x[2], y0, c[2]);
+        }
+    };
+    // 16 rows of keys or queries, as operands of the product with the state, and that
+    struct Rows {
+        uint4 v[PL ? NT / 2 : NT][PL ? KP : 1];
+    };
+    auto operands = [&](const Raw4<F32> (&x)[NT]) __attribute__((always_inline)) {
+        Rows rows;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if constexpr (!PL) {
+                rows.v[t][0] = make_uint4(x[t].w[0], x[t].w[1], x[t].w[2], x[t].w[3]);
+            } else if constexpr (F32) {
+                u2v v[3];
+                planes_of(x[t].get(), v);
+#pragma unroll
+                for (int i = 0; i < KP; ++i) {
+                    uint4& u = rows.v[t / 2][i];
+                    (t & 1 ? u.z : u.x) = v[i][0];
+                    (t & 1 ? u.w : u.y) = v[i][1];
+                }
+            } else {
+                uint4& u = rows.v[t / 2][0];
+                (t & 1 ? u.z : u.x) = x[t].w[0];
+                (t & 1 ? u.w : u.y) = x[t].w[1];
+            }
+        }
+        return rows;
+    };
+    auto rows_times_state = [&](const Rows& x) __attribute__((always_inline)) {
+        if constexpr (!PL) {
             // two sums: an instruction need not wait for the one before it
             f4v c[2] = {};
 #pragma unroll
-            for (int t = 0; t < NT; ++t) c[t & 1] = tile_product(x[t].get(), sbuf[t][lane], c[t & 1]);
+            for (int t = 0; t < NT; ++t) {
+                f4v v;
+                __builtin_memcpy(&v, &x.v[t][0], 16);
+                c[t & 1] = tile_product(v, sbuf[t][lane], c[t & 1]);
+            }
             return c[0] + c[1];
         } else {
             f4v c[3] = {};
 #pragma unroll
-            for (int t = 0; t < NT; t += 2) {
-                const uint4 v = make_uint4(x[t].w[0], x[t].w[1], x[t + 1].w[0], x[t + 1].w[1]);
-#pragma unroll
-                for (int i = 0; i < 3; ++i) c[i] = mfma_bf16(v, splanes[t / 2 * 3 + i][lane], c[i]);
-            }
+            for (int t = 0; t < NT / 2; ++t) plane_products(x.v[t], splanes + t * 3, c);
             return c[0] + (c[1] + c[2]);
         }
+    };
+    // 16 rows of keys into LDS, and as they lie there times the state
+    auto keep_keys = [&](const Raw4<F32> (&x)[NT], int tile, char* to) __attribute__((always_inline)) {
+        to += (16 * tile + r) * PITCH + 16 * g;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if constexpr (!PL) {
+                *(f4v*)(to + 64 * t) = x[t].get();
+            } else if constexpr (F32) {
+                u2v v[3];
+                planes_of(x[t].get(), v);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) *(u2v*)(to + i * PLANE + t / 2 * 64 + t % 2 * 8) = v[i];
+            } else {
+                *(u2v*)(to + t / 2 * 64 + t % 2 * 8) = u2v{x[t].w[0], x[t].w[1]};
+            }
+        }
+    };
+    auto keys_times_state = [&](int tile, const char* from) __attribute__((always_inline)) {
+        f4v c[3] = {};
+#pragma unroll
+        for (int t = 0; t < NT / 2; ++t) {
+            uint4 v[KP];
+#pragma unroll
+            for (int i = 0; i < KP; ++i) v[i] = *(const uint4*)(from + i * PLANE + (16 * tile + r) * PITCH + 64 * t + 16 * g);
+            plane_products(v, splanes + t * 3, c);
+        }
+        return c[0] + (c[1] + c[2]);
     };
     // the same from all of a workgroup's wavefronts
     auto bad_columns = [&]() __attribute__((always_inline)) {
         return __builtin_amdgcn_readfirstlane((bad[0] | bad[1] | bad[2] | bad[3]) & 0xFFFFu);
     };
     const int sums = a.unit ? 4 : 2;                   // of a token taken by itself
-    constexpr int HAND = F32 ? 0 : 1;                  // meeting before those, for the state in fp32
+    constexpr int HAND = PL ? 1 : 0;                   // meeting before those, for the state in fp32
 
     if (OUT && wave >= 4) {
         Raw4<F32> q[NT];
@@ -534,9 +608,22 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
 #pragma unroll
             for (int i = 0; i < 4; ++i) p[i] = *(const f4v*)((const char*)mu + off_p + (uint32_t)min(i, wq) * 1024);
         };
+        // and the next stretch's keys, loaded a stretch before they are cut
+        Raw4<F32> k[NT];
+        const char* from = (const char*)a.k + (row0 * a.ldk + hk * DK) * S;
+        const int64_t step_k = (int64_t)CHUNK * ldk;
+        auto load_k = [&](int c) __attribute__((always_inline)) {
+            const uint32_t off = (uint32_t)min(16 * w + r, tokens(c) - 1) * ldk + 4 * g * S;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) k[t].load(from + off + 16 * t * S, 0);
+        };
         if (chunks > c0) {
+            load_k(c0);
             load_q(c0);
             load_p();
+            keep_keys(k, w, kbuf + (c0 & 1) * KEYS);
+            if (c0 + 1 < chunks) from += step_k;
+            load_k(min(c0 + 1, chunks - 1));
         }
         const int64_t out_row = (int64_t)a.heads * DV;
         char* to = (char*)a.out + ((row0 + 16 * wq + 4 * g) * out_row + h * DV + col) * S;
@@ -548,11 +635,16 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
 #pragma unroll 1
         for (int c = c0; c < chunks; ++c) {
             const int m = tokens(c), next = min(c + 1, chunks - 1);
+            // beside the chain's first product
+            const Rows queries = operands(q);
+            keep_keys(k, w, kbuf + ((c + 1) & 1) * KEYS);
+            if (c + 2 < chunks) from += step_k;
+            load_k(min(c + 2, chunks - 1));
             lds_barrier();
             const uint32_t columns = bad_columns();
             if (columns)
                 for (int i = m * sums + HAND; i > 0; --i) lds_barrier();
-            f4v o[2] = {rows_times_state(q), {0.f, 0.f, 0.f, 0.f}};
+            f4v o[2] = {rows_times_state(queries), {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[0][e] *= fq[e];
             if (c + 1 < chunks) {
@@ -584,8 +676,8 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     f4v s[OWN];
     // for the products with it; and as it is, which a slow stretch and the parts before take
     auto give = [&](int t, const f4v v) __attribute__((always_inline)) {
-        if constexpr (F32) sbuf[t][lane] = v;
-        else cut(v, splanes, t);
+        if constexpr (PL) cut(v, splanes, t);
+        else sbuf[t][lane] = v;
     };
     auto tile = [&](int o) __attribute__((always_inline)) { return NT < 4 ? min(w, NT - 1) : w + 4 * o; };
     const bool own = NT >= 4 || w < NT;
@@ -606,7 +698,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             for (int e = 0; e < 4; ++e) s[o][e] = unit && 16 * tile(o) + 4 * g + e == col ? 1.f : 0.f;
         }
         if (own) sbuf[tile(o)][lane] = s[o];
-        if (!F32 && own) cut(s[o], splanes, tile(o));
+        if (PL && own) cut(s[o], splanes, tile(o));
     }
     Raw4<F32> k[NT];
     Raw1<F32> v[4];
@@ -626,8 +718,9 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
 #pragma unroll
             for (int e = 0; e < 4; ++e) off_v[e] = (uint32_t)min(16 * w + 4 * g + e, m - 1) * ldv + col * S;
         }
+        if constexpr (!OUT)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) k[t].load(keys + off_k + 16 * t * S, 0);
+            for (int t = 0; t < NT; ++t) k[t].load(keys + off_k + 16 * t * S, 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e].load(values + off_v[e], 0);
         fk = *(const f4v*)&mx[MATS_TOKEN + TOKEN_K * CHUNK + 16 * w + 4 * g];
@@ -654,7 +747,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         const bool raw = a.rate != nullptr;
         const float rate = raw ? a.rate[h] : 0.f, bias = raw ? a.bias[h] : 0.f;
         float z[R];
-        if constexpr (!F32) {
+        if constexpr (PL) {
 #pragma unroll
             for (int o = 0; o < OWN; ++o)
                 if (own) sbuf[tile(o)][lane] = s[o];
@@ -727,7 +820,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             for (int o = 0; o < OWN; ++o) {
                 s[o] = y[o];
                 if (own) sbuf[tile(o)][lane] = s[o];
-                if (!F32 && own) cut(s[o], splanes, tile(o));
+                if (PL && own) cut(s[o], splanes, tile(o));
             }
             lds_barrier();
         }
@@ -735,9 +828,14 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
 #pragma unroll 1
     for (int c = c0; c < chunks; ++c) {
         const int m = tokens(c), next = min(c + 1, chunks - 1);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) __builtin_memcpy(kbuf + (16 * w + r) * PITCH + (16 * t + 4 * g) * S, k[t].w, sizeof k[t].w);
-        f4v x = rows_times_state(k);
+        char* const kb = kbuf + (OUT ? (c & 1) * KEYS : 0);
+        f4v x;
+        if constexpr (OUT) {
+            x = keys_times_state(w, kb);
+        } else {
+            keep_keys(k, w, kb);
+            x = rows_times_state(operands(k));
+        }
         bool odd = keys_odd != 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -765,8 +863,8 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         if (OUT) ubuf[w][lane] = u[0];
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[0][e] *= fu[e];
-        if constexpr (F32) ybuf[w][lane] = u[0];
-        else cut(u[0], yplanes, w);
+        if constexpr (PL) cut(u[0], yplanes, w);
+        else ybuf[w][lane] = u[0];
 #pragma unroll
         for (int i = 0; i < OWN; ++i)
 #pragma unroll
@@ -774,42 +872,39 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         if (c + 1 < chunks) mu += step_m;
         load_u();
         lds_barrier();
-        f4v more[OWN] = {}, least[OWN] = {};
-        if constexpr (F32) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const f4v y = ybuf[t][lane];
-#pragma unroll
-                for (int i = 0; i < OWN; ++i) {
-                    f4v key;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) key[e] = *(const float*)(kbuf + (16 * t + 4 * g + e) * PITCH + (16 * tile(i) + r) * S);
-                    if (t & 1) more[i] = tile_product(key, y, more[i]);
-                    else s[i] = tile_product(key, y, s[i]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int t = 0; t < 4; t += 2)
-#pragma unroll
-                for (int i = 0; i < OWN; ++i) {
-                    // (a transposing read: 16 lanes take 4 rows of 16 keys' values, each lane a column of them)
-                    typedef short s4v __attribute__((ext_vector_type(4)));
-                    typedef __attribute__((address_space(3))) s4v lds_s4v;
-                    const lds_char* at = (const lds_char*)kbuf + (16 * t + 4 * g + (r >> 2)) * PITCH + (16 * tile(i) + 4 * (r & 3)) * S;
-                    const s4v k0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)at);
-                    const s4v k1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + 16 * PITCH));
-                    uint4 key;
-                    __builtin_memcpy(&key, &k0, 8);
-                    __builtin_memcpy((char*)&key + 8, &k1, 8);
-                    s[i] = mfma_bf16(key, yplanes[t / 2 * 3][lane], s[i]);
-                    more[i] = mfma_bf16(key, yplanes[t / 2 * 3 + 1][lane], more[i]);
-                    least[i] = mfma_bf16(key, yplanes[t / 2 * 3 + 2][lane], least[i]);
-                }
-        }
 #pragma unroll
         for (int i = 0; i < OWN; ++i) {
-            s[i] += F32 ? more[i] : more[i] + least[i];
+            if constexpr (!PL) {
+                f4v more = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    f4v key;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) key[e] = *(const float*)(kb + (16 * t + 4 * g + e) * PITCH + (16 * tile(i) + r) * 4);
+                    if (t & 1) more = tile_product(key, ybuf[t][lane], more);
+                    else s[i] = tile_product(key, ybuf[t][lane], s[i]);
+                }
+                s[i] += more;
+            } else {
+                // (a transposing read: 16 lanes take 4 rows of 16 keys' values, each lane a column of them)
+                typedef short s4v __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) s4v lds_s4v;
+                f4v sum[3] = {s[i]};
+                const lds_char* at = (const lds_char*)kb + (4 * g + (r >> 2)) * PITCH + tile(i) / 2 * 64 + (r & 3) * 16 + tile(i) % 2 * 8;
+#pragma unroll
+                for (int t = 0; t < 4; t += 2) {
+                    uint4 key[KP];
+#pragma unroll
+                    for (int p = 0; p < KP; ++p) {
+                        const s4v k0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + p * PLANE + 16 * t * PITCH));
+                        const s4v k1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v*)(at + p * PLANE + 16 * (t + 1) * PITCH));
+                        __builtin_memcpy(&key[p], &k0, 8);
+                        __builtin_memcpy((char*)&key[p] + 8, &k1, 8);
+                    }
+                    plane_products(key, yplanes + t / 2 * 3, sum);
+                }
+                s[i] = sum[0] + (sum[1] + sum[2]);
+            }
             if (columns >> r & 1) s[i] = zbuf[tile(i)][lane];
             if (own) give(tile(i), s[i]);
         }
