@@ -21,8 +21,10 @@
 //
 // so T = (I + A)^-1 and P are formed for all stretches at once (chunk_kernel), and what is
 // left from one to the next is five matrix products (state_kernel), each workgroup with 16
-// columns of a state.  They are products of fp32 values in the fp32 instructions: the state
-// that goes from stretch to stretch keeps its 24 bits.  A 16 x 16 result has its rows 4 g ..
+// columns of a state.  Those with T and P are products in the fp32 instructions; those with
+// keys, queries and the state go through the bf16 ones, sixteen times as fast, with an fp32
+// value cut into three bf16 planes that hold its 24 bits, and of the planes' products those
+// that an fp32 sum holds: three with bf16 keys, six with fp32 ones.  A 16 x 16 result has its rows 4 g ..
 // 4 g + 3 in lane 16 g + column, which is also where the next product wants its second
 // operand's rows if the first's columns come in the same order, so S, X and U pass from
 // product to product as they stand, between wavefronts through LDS.  Exponents are
@@ -430,10 +432,11 @@ __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
 // columns, the unit matrix through all parts but the last, without outputs, and the workgroups of the second begin with
 // the product of the parts before theirs.
 //
-// Bound by the way through a stretch: three products and meetings after one another, 2.3 us (523 stretches, four streams,
-// 8 fp32 heads of 64 x 128: 1190 us with 256 workgroups; 3348 tokens of 8 bf16 heads of 64 x 64 in eight parts: 23 and
-// 26).  W = T diag(beta e^G) K and T beta V formed for all stretches beforehand leave two (1064 us), and cost that time
-// there: 364 us for 205, and half as much memory again.
+// Bound by the way through a stretch: three products and meetings after one another, 2.1 us (523 stretches, four streams,
+// 8 fp32 heads of 64 x 128: 1090 us with 256 workgroups, with fp32 products throughout 1180; 3348 tokens of 8 bf16 heads
+// of 64 x 64 in eight parts: 19 and 22, 23 and 26).  Keys and queries are cut while the chain is at its first product; in
+// the second's time, cutting was 70 us more.  Matrices that come from memory later than a stretch after their loads are 70
+// us of it; touching them three stretches ahead, by the outputs' wavefronts or by a ninth, gave none of that back.
 template <bool F32, int DK, int DV, bool OUT>
 __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, const float* mats, float* parts) {
     constexpr int S = F32 ? 4 : 2;
@@ -853,12 +856,16 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         }
         load_x(next);
         lds_barrier();
+        // (read before the columns are known: a slow stretch leaves them)
+        f4v xs[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) xs[t] = xbuf[t][lane];
         const uint32_t columns = bad_columns();
         if (columns) slowly(c, columns);
         f4v u[2] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-            if (t <= w) u[t & 1] = tile_product(inv[t], xbuf[t][lane], u[t & 1]);
+            if (t <= w) u[t & 1] = tile_product(inv[t], xs[t], u[t & 1]);
         u[0] += u[1];
         if (OUT) ubuf[w][lane] = u[0];
 #pragma unroll
@@ -950,13 +957,15 @@ void launch_chunks(DeltaArgs a, int64_t slots, float* mats, hipStream_t s) {
 
 // Tokens one by one or in stretches, and the parts of the streams: whichever takes least by what the pieces take, in
 // microseconds.  A token is 0.35 and 0.0055 for each row of a head's state, or 0.45 for each thousand wavefronts where
-// there are many; a stretch with its outputs 2.5, without 1.6 (two workgroups on a compute unit), a product of parts 0.8; a
-// launch of states 1.5 for each round over the card, chunk_kernel 1 for 150 heads' stretches; the further launches 5 each.
-// (Heads of 64 x 64 in bf16, one by one and in stretches: 8 heads, 4 tokens 7.4 and 13.5, 16 tokens 16.0 and 13.6, 64
-// tokens 49 and 14; 128 heads, 16 tokens 16.4 and 19.0, 32 tokens 28 and 20; 8000 heads, 64 tokens 462 and 789, 128 tokens
-// 895 and 1114; 2400 heads of 32 x 32, 64 tokens 77 and 125.)
+// there are many; a stretch with its outputs 2.1 of bf16 and 2.9 of fp32 tokens (2.1 for a single round, more for many,
+// whose operands are memory's time), without 2 (two workgroups on a compute unit), a product of parts 0.8; a launch of
+// states 4 for each round over the card, chunk_kernel 1 for 150 heads' stretches, 80 of fp32; the further launches 5 each.
+// (Heads of 64 x 64 in bf16, one by one and in stretches: 8 heads, 8 tokens 10.2 and 13.2, 16 tokens 16.0 and 13.2, 64
+// tokens 49 and 14; 128 heads, 16 tokens 16.3 and 18.3, 32 tokens 27.6 and 18.8; 8000 heads, 64 tokens 462 and 715, 192
+// tokens 1329 and 1288; 4000 heads in fp32, 192 tokens 651 and 848; 2400 heads of 32 x 32, 64 tokens 76 and 118.)
 DeltaPlan delta_plan(const sscater_delta_memory* m, const sscater_token_rows* r) {
     DeltaPlan p = {0, 1, 0};
+    const bool f32 = m->dtype == SSCATER_F32;
     const double heads = (double)m->batch * m->heads, n = r->max_new, blocks = m->value_dim / 16;
     const double token = 5. + n * std::max(0.35 + 0.0055 * m->key_dim, 0.00045 * heads * blocks / 2.);
     const int64_t most = ((int64_t)r->max_new + CHUNK - 1) / CHUNK;
@@ -965,8 +974,8 @@ DeltaPlan delta_plan(const sscater_delta_memory* m, const sscater_token_rows* r)
         const int64_t length = (most + k - 1) / k;
         const double out = std::ceil(heads * blocks * k / 256.), in = std::ceil(heads * (blocks + m->key_dim / 16) * (k - 1) / 512.);
         if ((most + length - 1) / length != k || (k > 1 && out > 8.)) continue;
-        const double cost = 8. + heads * most / 150. + out * (1.5 + 2.5 * length) +
-                            (k > 1 ? 5. + in * (1.5 + 1.6 * length) + 0.8 * (k - 2) : 0.);
+        const double cost = 8. + heads * most / (f32 ? 80. : 150.) + out * (4. + (f32 ? 2.9 : 2.1) * length) +
+                            (k > 1 ? 5. + in * (4. + 2. * length) + 0.8 * (k - 2) : 0.);
         if (cost < best) {
             best = cost;
             p.slots = std::min((int64_t)r->tokens, (int64_t)r->max_new * m->batch) / CHUNK + m->batch;
