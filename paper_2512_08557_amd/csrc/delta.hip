@@ -433,7 +433,7 @@ __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
 // the product of the parts before theirs.
 //
 // Bound by the way through a stretch: three products and meetings after one another, 2.1 us (523 stretches, four streams,
-// 8 fp32 heads of 64 x 128: 1090 us with 256 workgroups, with fp32 products throughout 1180; 3348 tokens of 8 bf16 heads
+// 8 fp32 heads of 64 x 128: 1080 us with 256 workgroups, with fp32 products throughout 1180; 3348 tokens of 8 bf16 heads
 // of 64 x 64 in eight parts: 19 and 22, 23 and 26).  Keys and queries are cut while the chain is at its first product; in
 // the second's time, cutting was 70 us more.  Matrices that come from memory later than a stretch after their loads are 70
 // us of it; touching them three stretches ahead, by the outputs' wavefronts or by a ninth, gave none of that back.
@@ -561,19 +561,11 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     // 16 rows of keys into LDS, and as they lie there times the state
     auto keep_keys = [&](const Raw4<F32> (&x)[NT], int tile, char* to) __attribute__((always_inline)) {
         to += (16 * tile + r) * PITCH + 16 * g;
+        const Rows rows = operands(x);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if constexpr (!PL) {
-                *(f4v*)(to + 64 * t) = x[t].get();
-            } else if constexpr (F32) {
-                u2v v[3];
-                planes_of(x[t].get(), v);
+        for (int t = 0; t < (PL ? NT / 2 : NT); ++t)
 #pragma unroll
-                for (int i = 0; i < 3; ++i) *(u2v*)(to + i * PLANE + t / 2 * 64 + t % 2 * 8) = v[i];
-            } else {
-                *(u2v*)(to + t / 2 * 64 + t % 2 * 8) = u2v{x[t].w[0], x[t].w[1]};
-            }
-        }
+            for (int i = 0; i < (PL ? KP : 1); ++i) *(uint4*)(to + i * PLANE + 64 * t) = rows.v[t][i];
     };
     auto keys_times_state = [&](int tile, const char* from) __attribute__((always_inline)) {
         f4v c[3] = {};
