@@ -564,8 +564,9 @@ typedef struct {
  *   everything), beta = b;
  *   initial: states to begin from instead of memory->state, which is written all the
  *   same (a copy of it where a stream has no tokens), or NULL.
- * Everything is computed in fp32, tokens one by one or in stretches of 64, which
- * differ in their last bits; a stream's stretches are also what its tokens depend on:
+ * Everything is computed in fp32 (in stretches the products with keys, queries and
+ * the state from bf16 planes that hold its 24 bits, of values from 2^-110 on), tokens
+ * one by one or in stretches of 64, which differ in their last bits; a stream's stretches are also what its tokens depend on:
  * none on later ones, whatever those hold.  Rows behind the last stream's are left as
  * they were.  The workspace is as for attention. */
 int sscater_delta_workspace(const sscater_delta_spec* spec, const sscater_delta_memory* memory,
