@@ -566,8 +566,8 @@ typedef struct {
  *   same (a copy of it where a stream has no tokens), or NULL.
  * Everything is computed in fp32 (in stretches the products with keys, queries and
  * the state from bf16 planes that hold its 24 bits, of values from 2^-110 on), tokens
- * one by one or in stretches of 64, which differ in their last bits; a stream's stretches are also what its tokens depend on:
- * none on later ones, whatever those hold.  Rows behind the last stream's are left as
+ * one by one or in stretches of 64, which differ in their last bits.  No token
+ * depends on a later one, whatever that holds.  Rows behind the last stream's are left as
  * they were.  The workspace is as for attention. */
 int sscater_delta_workspace(const sscater_delta_spec* spec, const sscater_delta_memory* memory,
                             const sscater_token_rows* rows, size_t* bytes);
