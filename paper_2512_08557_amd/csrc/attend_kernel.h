@@ -76,7 +76,6 @@ struct AttendShape {
     // split once per workgroup on their way into LDS, through registers.
     static constexpr bool PL = F32 && WM == 4;
     static constexpr int NP = PL ? 3 : 1;          // planes
-    static constexpr int PP = PL ? 3 : !F32 && WM == 1 ? 2 : 1;   // parts of a probability
     static constexpr int LRB = PL ? D * 2 : RB;    // bytes of a row in LDS
     static constexpr int CPR = LRB / 16;           // its 16-byte pieces
     static constexpr bool B16 = !F32 || PL;        // bf16 operands
@@ -155,6 +154,7 @@ template <bool F32, int D, int WM, Keys SRC>
 __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_kernel(AttendArgs a) {
     using C = AttendShape<F32, D, WM>;
     constexpr bool CACHE = SRC == Keys::CACHE, LISTED = SRC == Keys::LISTED;
+    constexpr int PP = C::PL ? 3 : !F32 && WM == 1 ? 2 : 1;   // parts of a probability
     __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
     __shared__ float ml[4][32][2];
     // LISTED: the rows of each group's tiles j + 1 .. j + 3 (and j), copied as the tiles are
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                 for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
         }
         const float ms = m == -INFINITY ? 0.f : m;
-        uint4 pf[C::NT * 2][C::PP];                    // bf16 operands: eight probabilities each
+        uint4 pf[C::NT * 2][PP];                       // bf16 operands: eight probabilities each
         // the values of 16 keys (bf16 operands) or of two (fp32), all of a head
         constexpr int VS = C::B16 ? C::BN / 16 : 16, VA = C::B16 ? 2 : 4;
         Operand vf[VA][D / 32];
@@ -526,11 +526,11 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                         cut_pair(__float_as_uint(s[e >> 4][(e & 15) - 1]), __float_as_uint(x), w[0], w[1], w[2]);
                     else
                         w[0] = bf16_pair(s[e >> 4][(e & 15) - 1], x);
-                    if constexpr (C::PP == 2)
+                    if constexpr (PP == 2)
                         w[1] = bf16_pair(s[e >> 4][(e & 15) - 1] - __uint_as_float(w[0] << 16),
                                          x - __uint_as_float(w[0] & 0xFFFF0000u));
 #pragma unroll
-                    for (int p = 0; p < C::PP; ++p) {
+                    for (int p = 0; p < PP; ++p) {
                         uint4& f = pf[e >> 3][p];
                         if ((e & 7) == 1) f.x = w[p];
                         else if ((e & 7) == 3) f.y = w[p];
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
 #pragma unroll
             for (int t = 0; t < D / 32; ++t) {
                 const Operand& v = vf[ks % VA][t];
-                if constexpr (C::PP == 2) o[t] = mfma32(v.p[0], pf[ks][1], o[t]);
+                if constexpr (PP == 2) o[t] = mfma32(v.p[0], pf[ks][1], o[t]);
                 if constexpr (C::PL) o[t] = mfma_planes(v.p, pf[ks], o[t]);
                 else if constexpr (F32)
                     o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(v.p[0].x), s[0][ks], o[t], 0, 0, 0);
@@ -603,6 +603,16 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < 4; ++g) again |= ml[g][0][0] != 0.f;
+    }
+    if constexpr (PP == 2) {
+        // A probability's second part may be zero or negative, and an infinite value times that makes a sum NaN: such sums
+        // are formed again.
+        float any = 0.f;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) any += o[t][e];
+        again |= __ballot(any != any) != 0;
     }
     if (again) {
         // Keys one by one, each only for the rows that see it: the wavefront's
