@@ -518,6 +518,7 @@ typedef struct {
     int64_t q_stride, k_stride, v_stride;
     const int32_t* q_start;
     const int32_t* k_start;
+    int32_t rounded; /* 1: a bf16 call's probabilities may be rounded to bf16 */
 } sscater_cross_spec;
 
 /* out[i][h] = sum_j softmax_j(scale * q_i . k_j) v_j over the visible keys j of
@@ -525,9 +526,10 @@ typedef struct {
  * zeros where no key is visible.  mask: device bytes [keys], zero where a key is
  * not visible (its k and v are not read), or NULL; out: device [queries][q_heads]
  * [head_dim], on a 16-byte boundary.  Queries behind the last sequence's are left
- * as they were.  Precision as sscater_tokens_attend: scores, maxima and sums fp32;
- * bf16 probabilities are rounded to bf16 for their product with the values where a
- * sequence may bring more than 32 rows (max_q * q_heads / kv_heads).
+ * as they were.  Scores, maxima and sums are fp32; for their product with bf16 values
+ * probabilities are held in two bf16 parts (16 bits), or, with rounded = 1, rounded to
+ * bf16 where a sequence may bring more than 32 rows (max_q * q_heads / kv_heads): an
+ * error as large as the output's rounding, in some seven tenths of the time.
  * workspace: as there, sscater_cross_workspace() bytes (masked: also without
  * splits).  `masked`: whether there will be a mask. */
 int sscater_cross_workspace(const sscater_cross_spec* spec, int32_t masked, size_t* bytes);

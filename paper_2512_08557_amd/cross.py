@@ -52,7 +52,7 @@ _described = lru_cache(256)(_describe)
 
 
 def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional[int] = None,
-                 max_k: Optional[int] = None, scale: Optional[float] = None, out=None, stream=None):
+                 max_k: Optional[int] = None, scale: Optional[float] = None, out=None, stream=None, rounded: bool = False):
     """Attention of queries to the keys and values of another set of tokens (objects
     to a map's cells): softmax(scale * q k^T) v over the visible keys; zeros where a
     sequence has none.
@@ -66,9 +66,10 @@ def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional
     of one sequence, max_q and max_k, where they are known.  float32 or bfloat16,
     head_dim 32, 64 or 128, q_heads a multiple of kv_heads; rows may be columns of a
     projection's, evenly apart and on 16-byte boundaries.  scale: 1 / sqrt(head_dim)
-    unless given.  bfloat16: where a sequence may bring more than 32 rows (max_q *
-    q_heads / kv_heads) probabilities are rounded to bfloat16 for the product with the
-    values.  out: q's shape, contiguous, overlapping no operand."""
+    unless given.  out: q's shape, contiguous, overlapping no operand.  rounded
+    (bfloat16, where a sequence may bring more than 32 rows, max_q * q_heads / kv_heads):
+    probabilities rounded to bfloat16 for the product with the values, an error as large
+    as the output's rounding, in some seven tenths of the time."""
     if T.torch is None:
         T._bind()
     dtype = q.dtype
@@ -117,7 +118,7 @@ def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional
         return out
     spec, need = (_described if q_start is None else _describe)(
         0 if mask is None else 1, kind, batch, heads, k.shape[-2], dim, queries, keys, max_q, max_k,
-        dim ** -0.5 if scale is None else scale, ldq, ldk, ldv, *at)
+        dim ** -0.5 if scale is None else scale, ldq, ldk, ldv, *at, 1 if rounded else 0)
     work = q.new_empty(need, dtype=T.torch.uint8) if need else None
     T._launch(lib().sscater_cross_attend, "sscater_cross_attend", index, stream, (q, k, v, mask, q_start, k_start, out, work),
               spec, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if mask is None else mask.data_ptr(), out.data_ptr(),

@@ -35,10 +35,10 @@ void launch_attend(AttendArgs a, const AttendCut& cut, hipStream_t s) {
         a.id0 = (int)at;
         const dim3 grid((unsigned)std::min(LAUNCH_GROUPS, cut.grid - at));
         if constexpr (!(F32 && D == 128)) {
-            if (cut.wm == 1) attend_kernel<F32, D, 1, Keys::CACHE><<<grid, block, 0, s>>>(a);
+            if (cut.wm == 1) attend_kernel<F32, D, 1, Keys::CACHE, false><<<grid, block, 0, s>>>(a);
         }
-        if (cut.wm == 2) attend_kernel<F32, D, 2, Keys::CACHE><<<grid, block, 0, s>>>(a);
-        if (cut.wm == 4) attend_kernel<F32, D, 4, Keys::CACHE><<<grid, block, 0, s>>>(a);
+        if (cut.wm == 2) attend_kernel<F32, D, 2, Keys::CACHE, !F32><<<grid, block, 0, s>>>(a);
+        if (cut.wm == 4) attend_kernel<F32, D, 4, Keys::CACHE, !F32><<<grid, block, 0, s>>>(a);
     }
     if (cut.splits > 1) {                              // at most some hundred thousand rows: see cut_keys
         const int64_t rows = (int64_t)a.rows.tokens * a.q_heads;

@@ -20,10 +20,13 @@
 // of a key head are bound by the cache's bytes and take them in two parts, which
 // hold 16 bits (one token of sixteen streams over 65536 keys 358 us, with one part
 // 358; eight tokens over 16384 keys 27.5, 26.9): the error is that of the output's
-// rounding alone.  More rows are bound by the products and take one part, an error
-// as large as the output's rounding (a window of 33480 tokens 1920 us, in two
-// parts 2680; 48 rows over 16384 keys 30.9 and 33.1).  The sum is of the
-// unrounded probabilities.
+// rounding alone.  More rows are bound by the products.  Of the cache they take one
+// part, an error as large as the output's rounding (a window of 33480 tokens 1920
+// us, in two parts 2680; 48 rows over 16384 keys 30.9 and 33.1); of another set of
+// tokens two, and one where the caller asks for it (900 queries of four maps of
+// 53568 cells, 16 heads of 64 on 4: 1440 us, in one part 1010; 8 heads of 32, a
+// quarter of the cells visible: 161 and 117; 500 queries over two times 20000 keys,
+// 8 heads of 128 on 4: 132 and 100).  The sum is of the unrounded probabilities.
 //
 // WM of the four wavefronts share keys and take different rows, the other
 // 4 / WM groups take other tiles of keys and are joined at the end.  Where the
@@ -150,11 +153,12 @@ __device__ __forceinline__ f16v mfma_planes(const uint4 (&x)[3], const uint4 (&y
     return mfma32(x[0], y[0], c);
 }
 
-template <bool F32, int D, int WM, Keys SRC>
+// ONE: bf16 probabilities in one part, whatever the rows
+template <bool F32, int D, int WM, Keys SRC, bool ONE>
 __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_kernel(AttendArgs a) {
     using C = AttendShape<F32, D, WM>;
     constexpr bool CACHE = SRC == Keys::CACHE, LISTED = SRC == Keys::LISTED;
-    constexpr int PP = C::PL ? 3 : !F32 && WM == 1 ? 2 : 1;   // parts of a probability
+    constexpr int PP = C::PL ? 3 : F32 || ONE ? 1 : 2;   // parts of a probability
     __shared__ __attribute__((aligned(1024))) char lds[C::LDS];
     __shared__ float ml[4][32][2];
     // LISTED: the rows of each group's tiles j + 1 .. j + 3 (and j), copied as the tiles are
@@ -301,8 +305,10 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
 #pragma unroll
             for (int i = 0; i < C::NC; ++i) {
                 const int r = i * (WM * C::RPC) + row0;
-                copy16(from + (uint32_t)(r * pitch + (pc ^ (V ? C::swap_v(r) : C::swap_k(r))) * 16),
-                       to + (i * WM + wm) * 1024);
+                const uint32_t at = (pc ^ (V ? C::swap_v(r) : C::swap_k(r))) * 16;
+                // (rows evenly apart: a scalar from copy to copy, and one offset for a lane)
+                if constexpr (CACHE) copy16(from + (uint32_t)(r * pitch + at), to + (i * WM + wm) * 1024);
+                else copy16(from + (int64_t)(i * (WM * C::RPC)) * pitch + (uint32_t)(row0 * pitch + at), to + (i * WM + wm) * 1024);
             }
         } else {
 #pragma unroll (LISTED ? C::NC : 1)

@@ -6,10 +6,10 @@
 // ones: their rows' numbers, one behind the other, are all that the attention looks
 // at, and cells that are not visible cost nothing but their byte of the mask.
 //
-// Bound by the softmax's vector instructions for heads of 32 (3600 queries, a quarter
-// of four times 53568 cells visible, 8 bf16 heads: 114 us, matrix cores 19 % busy), by
-// those and the products for larger ones (all cells, 16 heads of 64 on 4: 980 us, 806
-// TFLOP/s, 35 % busy).
+// Bound by the softmax's vector instructions and the products with the values, twice as
+// many as with the keys (3600 queries, a quarter of four times 53568 cells visible, 8
+// bf16 heads of 32: 161 us; all cells, 16 heads of 64 on 4: 1440 us, 550 TFLOP/s of the
+// formula's; with probabilities rounded to bf16 117 and 1010).
 #include "attend_kernel.h"
 
 #include <algorithm>
@@ -94,7 +94,7 @@ bool cross_plan(const sscater_cross_spec* s, bool masked, CrossPlan* p) {
     if (s->batch < 1 || s->batch > (1 << 24) || s->kv_heads < 1 || s->q_heads < 1 || s->q_heads > (1 << 16) ||
         s->q_heads % s->kv_heads || (s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128))
         return false;
-    if (!(s->scale == s->scale) || (s->q_start == nullptr) != (s->k_start == nullptr) || (uintptr_t)s->q_start % 4 ||
+    if (!(s->scale == s->scale) || s->rounded < 0 || s->rounded > 1 || (s->q_start == nullptr) != (s->k_start == nullptr) || (uintptr_t)s->q_start % 4 ||
         (uintptr_t)s->k_start % 4)
         return false;
     auto rows_ok = [&](int64_t all, int64_t most) {
@@ -119,17 +119,17 @@ bool cross_plan(const sscater_cross_spec* s, bool masked, CrossPlan* p) {
     return true;
 }
 
-template <bool F32, int D, Keys SRC>
+template <bool F32, int D, Keys SRC, bool ONE>
 void launch_cross(AttendArgs a, const AttendCut& cut, hipStream_t s) {
     const dim3 block(256);
     for (int64_t at = 0; at < cut.grid; at += LAUNCH_GROUPS) {
         a.id0 = (int)at;
         const dim3 grid((unsigned)std::min(LAUNCH_GROUPS, cut.grid - at));
-        if constexpr (!(F32 && D == 128)) {
-            if (cut.wm == 1) attend_kernel<F32, D, 1, SRC><<<grid, block, 0, s>>>(a);
+        if constexpr (!(F32 && D == 128) && !ONE) {
+            if (cut.wm == 1) attend_kernel<F32, D, 1, SRC, false><<<grid, block, 0, s>>>(a);
         }
-        if (cut.wm == 2) attend_kernel<F32, D, 2, SRC><<<grid, block, 0, s>>>(a);
-        if (cut.wm == 4) attend_kernel<F32, D, 4, SRC><<<grid, block, 0, s>>>(a);
+        if (cut.wm == 2) attend_kernel<F32, D, 2, SRC, ONE><<<grid, block, 0, s>>>(a);
+        if (cut.wm == 4) attend_kernel<F32, D, 4, SRC, ONE><<<grid, block, 0, s>>>(a);
     }
     if (cut.splits > 1) {                              // at most some hundred thousand rows: see cut_keys
         const int64_t rows = (int64_t)a.rows.tokens * a.q_heads;
@@ -138,11 +138,18 @@ void launch_cross(AttendArgs a, const AttendCut& cut, hipStream_t s) {
     }
 }
 
-template <bool F32, Keys SRC>
+template <bool F32, Keys SRC, bool ONE>
 void launch_cross(const AttendArgs& a, const AttendCut& cut, int dim, hipStream_t s) {
-    if (dim == 32) launch_cross<F32, 32, SRC>(a, cut, s);
-    else if (dim == 64) launch_cross<F32, 64, SRC>(a, cut, s);
-    else launch_cross<F32, 128, SRC>(a, cut, s);
+    if (dim == 32) launch_cross<F32, 32, SRC, ONE>(a, cut, s);
+    else if (dim == 64) launch_cross<F32, 64, SRC, ONE>(a, cut, s);
+    else launch_cross<F32, 128, SRC, ONE>(a, cut, s);
+}
+
+template <Keys SRC>
+void launch_cross(const AttendArgs& a, const AttendCut& cut, bool f32, bool one, int dim, hipStream_t s) {
+    if (f32) launch_cross<true, SRC, false>(a, cut, dim, s);
+    else if (one && cut.wm > 1) launch_cross<false, SRC, true>(a, cut, dim, s);
+    else launch_cross<false, SRC, false>(a, cut, dim, s);
 }
 
 }  // namespace
@@ -197,13 +204,9 @@ int sscater_cross_attend(const sscater_cross_spec* spec, const void* q, const vo
             list_kernel<<<dim3((unsigned)std::min(LAUNCH, groups - id)), dim3(1024), 0, (hipStream_t)stream>>>(
                 mask, keys, list, list + p.keys, (int)parts, id);
     }
-    if (f32) {
-        if (listed) launch_cross<true, Keys::LISTED>(a, p.cut, spec->head_dim, (hipStream_t)stream);
-        else launch_cross<true, Keys::ROWS>(a, p.cut, spec->head_dim, (hipStream_t)stream);
-    } else {
-        if (listed) launch_cross<false, Keys::LISTED>(a, p.cut, spec->head_dim, (hipStream_t)stream);
-        else launch_cross<false, Keys::ROWS>(a, p.cut, spec->head_dim, (hipStream_t)stream);
-    }
+    const bool one = spec->rounded != 0;
+    if (listed) launch_cross<Keys::LISTED>(a, p.cut, f32, one, spec->head_dim, (hipStream_t)stream);
+    else launch_cross<Keys::ROWS>(a, p.cut, f32, one, spec->head_dim, (hipStream_t)stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SSCATER_OK : report_hip_error(e);
 }

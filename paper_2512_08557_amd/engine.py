@@ -106,7 +106,8 @@ class CrossSpec(ctypes.Structure):
                 ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("queries", ctypes.c_int32),
                 ("keys", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_k", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
-                ("v_stride", ctypes.c_int64), ("q_start", ctypes.c_void_p), ("k_start", ctypes.c_void_p)]
+                ("v_stride", ctypes.c_int64), ("q_start", ctypes.c_void_p), ("k_start", ctypes.c_void_p),
+                ("rounded", ctypes.c_int32)]
 
 
 class DeltaMemorySpec(ctypes.Structure):

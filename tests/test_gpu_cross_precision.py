@@ -80,3 +80,40 @@ def test_an_infinite_value_of_few_rows(dim, form, rows):
     rest = torch.ones(ref[0].shape, dtype=torch.bool)
     rest[:, 0, 3] = rest[:, 1, 7] = False
     close(out, *ref, "the other values", rest)
+
+
+@pytest.mark.parametrize("visible", [None, 0.5])
+@pytest.mark.parametrize("queries,group,keys", [(33, 1, 700), (64, 1, 64), (20, 3, 1500), (65, 1, 4096), (130, 2, 333), (300, 1, 9001)])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_many_bf16_rows_are_off_by_the_rounding_of_the_output_alone(dim, queries, group, keys, visible):
+    """More than 32 rows of a key head, up to 64 and more; rounded=True: a probability is off by 2^-8."""
+    note(f"[gpu-test] cross {queries} x {group} rows, {keys} keys of {dim}, visible {visible}")
+    rng = np.random.default_rng(keys + dim)
+    q, k, v = normal(rng, (queries, 2 * group, dim), 2.0), normal(rng, (keys, 2, dim)), normal(rng, (keys, 2, dim))
+    seen = None if visible is None else torch.from_numpy(rng.random(keys) < visible).cuda()
+    close(ssc.cross_attend(q, k, v, seen), *reference(q, k, v, seen), "two parts")
+    close(ssc.cross_attend(q, k, v, seen, rounded=True), *reference(q, k, v, seen, 2.0 ** -8), "rounded")
+
+
+@pytest.mark.parametrize("rounded", [False, True])
+@pytest.mark.parametrize("rows", [33, 64, 130])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_an_infinite_value_of_many_rows(dim, rows, rounded):
+    note(f"[gpu-test] infinite values, {rows} rows of {dim}, rounded {rounded}")
+    rng = np.random.default_rng(rows + dim)
+    q, k, v = normal(rng, (rows, 2, dim), 2.0), normal(rng, (192, 2, dim)), normal(rng, (192, 2, dim))
+    ref = reference(q, k, v, None, 2.0 ** -8 if rounded else 2.0 ** -16)
+    v[50, 0, 3], v[60, 1, 7] = math.inf, -math.inf
+    out = ssc.cross_attend(q, k, v, rounded=rounded)
+    assert bool((out[:, 0, 3] == math.inf).all()) and bool((out[:, 1, 7] == -math.inf).all())
+    rest = torch.ones(ref[0].shape, dtype=torch.bool)
+    rest[:, 0, 3] = rest[:, 1, 7] = False
+    close(out, *ref, "the other values", rest)
+
+
+def test_where_nothing_is_rounded():
+    """float32, and up to 32 rows: the same bits either way."""
+    rng = np.random.default_rng(3)
+    for kind, queries in ((torch.float32, 100), (torch.float32, 5), (BF16, 32), (BF16, 1)):
+        q, k, v = (normal(rng, (n, 2, 64)).to(kind) for n in (queries, 500, 500))
+        assert torch.equal(ssc.cross_attend(q, k, v), ssc.cross_attend(q, k, v, rounded=True))
