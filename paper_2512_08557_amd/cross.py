@@ -118,7 +118,7 @@ def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional
         return out
     spec, need = (_described if q_start is None else _describe)(
         0 if mask is None else 1, kind, batch, heads, k.shape[-2], dim, queries, keys, max_q, max_k,
-        dim ** -0.5 if scale is None else scale, ldq, ldk, ldv, *at, 1 if rounded else 0)
+        dim ** -0.5 if scale is None else T._number(scale), ldq, ldk, ldv, *at, 1 if rounded else 0)
     work = q.new_empty(need, dtype=T.torch.uint8) if need else None
     T._launch(lib().sscater_cross_attend, "sscater_cross_attend", index, stream, (q, k, v, mask, q_start, k_start, out, work),
               spec, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if mask is None else mask.data_ptr(), out.data_ptr(),

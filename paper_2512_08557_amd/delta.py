@@ -117,8 +117,8 @@ class DeltaMemory:
             out = q.new_empty(shape)
         elif T._dense(out, "out", self.kind, index, shape) % 16:
             raise ValueError("out must be on a 16-byte boundary")
-        spec = E.DeltaSpec(0 if eps is None else 1, 0.0 if eps is None else eps,
-                           self.key_dim ** -0.5 if scale is None else scale, ldq, ldk, ldv, lda, ldb)
+        spec = E.DeltaSpec(0 if eps is None else 1, 0.0 if eps is None else T._number(eps),
+                           self.key_dim ** -0.5 if scale is None else T._number(scale), ldq, ldk, ldv, lda, ldb)
         need, work = ctypes.c_size_t(), None
         _check(lib().sscater_delta_workspace(spec, self._spec, rows, need), "sscater_delta_workspace")
         if need.value:

@@ -70,8 +70,8 @@ def _call(x, block, block_norm, block_weight, block_bias, gate, activation, scal
             raise ValueError("total and out must be two tensors")
     else:
         y, ldy = None if weight is None else block.new_empty(shape), width
-    spec = _spec(rows, shared, width, T._KINDS[dtype], 1 if center else 0, 1 if block_norm else 0, act, eps, ldx, ldb, ldg,
-                 lds, ldy)
+    spec = _spec(rows, shared, width, T._KINDS[dtype], 1 if center else 0, 1 if block_norm else 0, act, T._number(eps), ldx,
+                 ldb, ldg, lds, ldy)
     T._launch(lib().sscater_norm, "sscater_norm", index, stream,
               (x, block, gate, total, y, block_weight, block_bias, scale, weight, bias), spec,
               None if x is None else x.data_ptr(), block.data_ptr(), _width(block_weight, "block_weight", dtype, index, width),

@@ -60,6 +60,16 @@ def _want_gradient() -> None:
         raise ValueError("no gradient is formed: detach the operands or call under torch.no_grad()")
 
 
+def _number(value) -> float:
+    """A scale or an eps as a plain number: of a tensor what it holds now (descriptions of
+    calls are kept by their values, and a tensor is found by what it is, not holds)."""
+    if type(value) is float:
+        return value
+    if getattr(value, "requires_grad", False):
+        _want_gradient()
+    return float(value)
+
+
 def _launch(fn, where: str, index: int, stream, tensors, *args) -> None:
     """One library call on device `index`, on torch's current stream; another
     stream first waits for that one, and the call's tensors are recorded there
@@ -269,7 +279,7 @@ class TokenCache:
             out = qkv.new_empty(shape)
         else:
             _dense(out, "out", self.kind, index, shape)
-        spec = E.HeadSpec(q_heads, axes, rotary.section, rotary.interleaved, eps, ld)
+        spec = E.HeadSpec(q_heads, axes, rotary.section, rotary.interleaved, _number(eps), ld)
         _launch(lib().sscater_tokens_append, "sscater_tokens_append", index, stream,
                 (qkv, pos, rotary.inv_freq, q_weight, k_weight, start, out, self.k, self.v, self.past), spec,
                 self._spec, rows, qkv.data_ptr(), qw, kw, freq, at, out.data_ptr())
@@ -300,7 +310,7 @@ class TokenCache:
         elif _dense(out, "out", self.kind, index, q.shape) % 16:
             raise ValueError("out must be on a 16-byte boundary")
         spec = E.AttendSpec(q.shape[1], min(int(window), 2 ** 31 - 1), 1 if causal else 0,
-                            self.head_dim ** -0.5 if scale is None else scale)
+                            self.head_dim ** -0.5 if scale is None else _number(scale))
         cache, need, work = self._spec, ctypes.c_size_t(), None
         _check(lib().sscater_tokens_workspace(spec, cache, rows, need), "sscater_tokens_workspace")
         if need.value:
