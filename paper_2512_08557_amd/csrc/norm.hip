@@ -435,7 +435,8 @@ extern "C" int sscater_norm(const sscater_norm_spec* spec, const void* x, const 
                             const void* bias, void* sum, void* y, void* stream) {
     if (!spec || (spec->dtype != SSCATER_F32 && spec->dtype != SSCATER_BF16)) return SSCATER_E_INVALID_ARG;
     const int64_t C = spec->width, rows = spec->rows;
-    if (rows < 0 || rows > (int64_t(1) << 36) || C < 1 || C > (1 << 30) || rows * C > (int64_t(1) << 40))
+    // (the quotient: a product of both limits would pass 64 bits)
+    if (rows < 0 || rows > (int64_t(1) << 36) || C < 1 || C > (1 << 30) || (rows > 0 && C > (int64_t(1) << 40) / rows))
         return SSCATER_E_INVALID_ARG;
     if (spec->center < 0 || spec->center > 1 || spec->block_norm < 0 || spec->block_norm > 1 || !(spec->eps >= 0.f) ||
         (spec->activation != SSCATER_ACT_NONE && spec->activation != SSCATER_ACT_SILU &&
