@@ -114,6 +114,8 @@ def cross_attend(q, k, v, mask=None, q_start=None, k_start=None, max_q: Optional
         out = q.new_empty(q.shape)
     elif T._dense(out, "out", dtype, index, q.shape) % 16:
         raise ValueError("out must be on a 16-byte boundary")
+    elif out.requires_grad:
+        T._want_gradient()
     if queries == 0:
         return out
     spec, need = (_described if q_start is None else _describe)(

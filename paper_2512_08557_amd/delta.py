@@ -86,6 +86,8 @@ class DeltaMemory:
         sqrt(key_dim) unless given.  initial: states to begin from instead of the
         memory's (which are written all the same)."""
         index = self.index
+        if self._state.requires_grad:
+            T._want_gradient()
         if q.dim() != 3:
             raise ValueError("q must be [tokens, qk_heads, key_dim]")
         tokens = q.shape[0]
@@ -117,6 +119,8 @@ class DeltaMemory:
             out = q.new_empty(shape)
         elif T._dense(out, "out", self.kind, index, shape) % 16:
             raise ValueError("out must be on a 16-byte boundary")
+        elif out.requires_grad:
+            T._want_gradient()
         spec = E.DeltaSpec(0 if eps is None else 1, 0.0 if eps is None else T._number(eps),
                            self.key_dim ** -0.5 if scale is None else T._number(scale), ldq, ldk, ldv, lda, ldb)
         need, work = ctypes.c_size_t(), None

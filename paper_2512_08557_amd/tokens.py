@@ -55,7 +55,8 @@ def _dense(t, name: str, dtype, index: int, shape):
 
 def _want_gradient() -> None:
     """Called for operands that require a gradient: a result without one would be
-    taken for a constant."""
+    taken for a constant; and for tensors that are written and require one: what
+    autograd holds of them would not know of it."""
     if torch.is_grad_enabled():
         raise ValueError("no gradient is formed: detach the operands or call under torch.no_grad()")
 
@@ -153,6 +154,8 @@ def linear(x, weight, bias=None, activation: Optional[str] = None, residual=None
         out, ys = x.new_empty(shape), cout
     else:
         ys = _row_stride(_require(out, "out", dtype, index, shape), "out", cout)
+        if out.requires_grad:
+            _want_gradient()
     spec = E.LinearSpec(x.numel() // cin, cin, cout, kind, act, xs, ws, rs, ys)
     _launch(lib().sscater_linear, "sscater_linear", index, stream, (x, weight, bias, residual, out), spec, x.data_ptr(),
             weight.data_ptr(), None if bias is None else bias.data_ptr(),
@@ -271,7 +274,7 @@ class TokenCache:
             qw, kw = (_dense(w, "q_weight and k_weight", self.kind, index, (dim,)) for w in (q_weight, k_weight))
             if q_weight.requires_grad or k_weight.requires_grad:
                 _want_gradient()
-        if qkv.requires_grad:
+        if qkv.requires_grad or self._k.requires_grad or self._v.requires_grad:
             _want_gradient()
         rows = self._rows(tokens, start, max_new)
         shape = (tokens, q_heads, dim)
@@ -279,6 +282,8 @@ class TokenCache:
             out = qkv.new_empty(shape)
         else:
             _dense(out, "out", self.kind, index, shape)
+            if out.requires_grad:
+                _want_gradient()
         spec = E.HeadSpec(q_heads, axes, rotary.section, rotary.interleaved, _number(eps), ld)
         _launch(lib().sscater_tokens_append, "sscater_tokens_append", index, stream,
                 (qkv, pos, rotary.inv_freq, q_weight, k_weight, start, out, self.k, self.v, self.past), spec,
@@ -302,13 +307,15 @@ class TokenCache:
             raise ValueError("q must be contiguous, on a 16-byte boundary")
         if window < 1:
             raise ValueError("window must be at least 1")
-        if q.requires_grad:
+        if q.requires_grad or self._k.requires_grad or self._v.requires_grad:
             _want_gradient()
         rows = self._rows(q.shape[0], start, max_new)
         if out is None:
             out = q.new_empty(q.shape)
         elif _dense(out, "out", self.kind, index, q.shape) % 16:
             raise ValueError("out must be on a 16-byte boundary")
+        elif out.requires_grad:
+            _want_gradient()
         spec = E.AttendSpec(q.shape[1], min(int(window), 2 ** 31 - 1), 1 if causal else 0,
                             self.head_dim ** -0.5 if scale is None else _number(scale))
         cache, need, work = self._spec, ctypes.c_size_t(), None
