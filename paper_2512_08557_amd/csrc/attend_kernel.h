@@ -288,8 +288,8 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
     };
     // row r of tile t, of round j, which need not be whole
     auto row_of = [&](int t, int j, int r) __attribute__((always_inline)) -> int64_t {
-        // (sequences that overlap, against the call's contract, write over one another's lists)
-        if constexpr (LISTED) return min(named[wk][j & 3][r], k_last);
+        // (sequences that overlap, against the call's contract, write over one another's lists, or leave some unwritten)
+        if constexpr (LISTED) return min(max(named[wk][j & 3][r], 0), k_last);
         const int u = min(t * C::BN + r, reach.total - 1);
         if constexpr (CACHE) return slot_of(a, reach, u);
         return u;
@@ -633,7 +633,7 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
             if ((u / C::BN - tb) % C::WK != wk || !(u <= last && (u >= from || u < a.sinks))) continue;
             int64_t at = u;
             if constexpr (CACHE) at = slot_of(a, reach, u);
-            if constexpr (LISTED) at = min(a.list[k_first + u], k_last);
+            if constexpr (LISTED) at = min(max(a.list[k_first + u], 0), k_last);
             float x = 0.f;
 #pragma unroll 1
             for (int c = 0; c < C::RB / 16; ++c) {

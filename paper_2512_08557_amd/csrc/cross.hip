@@ -4,7 +4,8 @@
 //
 // Keys have no order, so the visible ones of a sequence may as well be the only
 // ones: their rows' numbers, one behind the other, are all that the attention looks
-// at, and cells that are not visible cost nothing but their byte of the mask.
+// at, and cells that are not visible cost nothing but the reading of their byte of the
+// mask.
 //
 // Bound by the softmax's vector instructions and the products with the values, twice as
 // many as with the keys (3600 queries, a quarter of four times 53568 cells visible, 8
@@ -26,20 +27,105 @@ __device__ __forceinline__ uint32_t seen4(uint32_t w) {
     return x * 0x00204081u >> 28;
 }
 
+// The sequence and the part of it that workgroup `slot` has, where sequence b's parts are first / LIST_KEYS + b onwards, as
+// many as it needs at most; false: none.
+__device__ __forceinline__ int list_slot(int first, int b) { return first / LIST_KEYS + b; }
+
+__device__ __forceinline__ bool list_part(const TokenRows& keys, int slot, int& b, int& part, int& first, int& n) {
+    int lo = 0, hi = keys.batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        rows_of(keys, mid, first, n);
+        if (list_slot(first, mid) <= slot) lo = mid; else hi = mid - 1;
+    }
+    b = lo;
+    rows_of(keys, b, first, n);
+    const int p = slot - list_slot(first, b);
+    if (p < 0 || p >= (n + LIST_KEYS - 1) / LIST_KEYS) return false;
+    part = p * LIST_KEYS;
+    return true;
+}
+
+// How many keys of a part are visible.
+__global__ __launch_bounds__(256) void count_kernel(const uint8_t* mask, TokenRows keys, int32_t* counts, int64_t id0) {
+    __shared__ int sums[4];
+    const int slot = (int)(id0 + blockIdx.x), t = threadIdx.x;
+    int b, part, first, n;
+    if (!list_part(keys, slot, b, part, first, n)) return;
+    mask += first;
+    const int at = part + 16 * t;
+    int seen = 0;
+    if (at + 16 <= n) {
+        uint32_t w[4];
+        __builtin_memcpy(w, mask + at, 16);
+        seen = __popc(seen4(w[0])) + __popc(seen4(w[1])) + __popc(seen4(w[2])) + __popc(seen4(w[3]));
+    } else {
+        for (int i = at; i < n; ++i) seen += mask[i] != 0;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) seen += __shfl_xor(seen, o);
+    if ((t & 63) == 0) sums[t >> 6] = seen;
+    __syncthreads();
+    if (t == 0) counts[slot] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+
+// The counts of a sequence's parts made those of the parts before, a wavefront a sequence, four parts a lane; and the
+// sequence's own.
+__global__ __launch_bounds__(256) void before_kernel(TokenRows keys, int32_t* counts, int32_t* count) {
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (id >= keys.batch) return;
+    int first, n;
+    rows_of(keys, (int)id, first, n);
+    const int parts = (n + LIST_KEYS - 1) / LIST_KEYS;
+    counts += list_slot(first, (int)id);
+    uint32_t all = 0;
+    for (int i = 4 * lane; i - 4 * lane < parts; i += 256) {
+        uint32_t c[4], mine = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            c[e] = i + e < parts ? (uint32_t)counts[i + e] : 0;
+            mine += c[e];
+        }
+        uint32_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t v = __shfl_up(upto, o);
+            if (lane >= o) upto += v;
+        }
+        uint32_t before = all + upto - mine;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (i + e < parts) counts[i + e] = (int)before;
+            before += c[e];
+        }
+        all += __shfl(upto, 63);
+    }
+    if (lane == 0) count[id] = (int)min(all, (uint32_t)n);
+}
+
 // A sequence's visible keys in order.  Workgroup b * parts + p lists those among the p-th
-// LIST_KEYS of sequence b, behind the ones before them, which it counts itself, 16 bytes a
-// lane: a second launch would take longer than reading a mask again (four maps of 53568
-// cells 5 us).
+// LIST_KEYS of sequence b, behind the ones before them.  Of few parts it counts those
+// itself, 16 bytes a lane: further launches would take longer than reading a mask again
+// (four maps of 53568 cells 5 us).  COUNTED: of many the two kernels above have, and
+// workgroup `slot` has what list_part() says.
+template <bool COUNTED>
 __global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRows keys, int32_t* list, int32_t* count,
-                                                    int parts, int64_t id0) {
+                                                    const int32_t* counts, int parts, int64_t id0) {
     __shared__ int sums[2][16];
     const int64_t id = id0 + blockIdx.x;
-    const int b = (int)(id / parts), t = threadIdx.x;
-    int first, n;
-    rows_of(keys, b, first, n);
-    const int part = (int)(id % parts) * LIST_KEYS, at = part + 4 * t;
-    if (part >= n && part > 0) return;
+    const int t = threadIdx.x;
+    int b, part, first, n;
+    if constexpr (COUNTED) {
+        if (!list_part(keys, (int)id, b, part, first, n)) return;
+    } else {
+        b = (int)(id / parts);
+        part = (int)(id % parts) * LIST_KEYS;
+        rows_of(keys, b, first, n);
+        if (part >= n && part > 0) return;
+    }
     mask += first;
+    const int at = part + 4 * t;
     uint32_t word = 0;
     if (at + 4 <= n) {
         __builtin_memcpy(&word, mask + at, 4);
@@ -47,18 +133,20 @@ __global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRo
         for (int i = 0; at + i < n; ++i) word |= (uint32_t)mask[at + i] << (8 * i);
     }
     int before = 0;
+    if constexpr (!COUNTED) {
 #pragma unroll 4
-    for (int i = t * 16; i < part; i += 16 * 1024) {
-        uint32_t w[4];
-        __builtin_memcpy(w, mask + i, 16);
-        before += __popc(seen4(w[0])) + __popc(seen4(w[1])) + __popc(seen4(w[2])) + __popc(seen4(w[3]));
+        for (int i = t * 16; i < part; i += 16 * 1024) {
+            uint32_t w[4];
+            __builtin_memcpy(w, mask + i, 16);
+            before += __popc(seen4(w[0])) + __popc(seen4(w[1])) + __popc(seen4(w[2])) + __popc(seen4(w[3]));
+        }
     }
     const uint32_t bits = seen4(word);
     const int mine = __popc(bits);
     int upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        before += __shfl_xor(before, o);
+        if constexpr (!COUNTED) before += __shfl_xor(before, o);
         const int v = __shfl_up(upto, o);
         if ((t & 63) >= o) upto += v;
     }
@@ -68,6 +156,8 @@ __global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRo
     }
     __syncthreads();
     int base = 0, all = 0;
+    // (sequences that overlap, against the call's contract, count over one another's parts)
+    if constexpr (COUNTED) base = min(max(counts[id], 0), part);
 #pragma unroll
     for (int w = 0; w < 16; ++w) {
         base += sums[0][w] + (w < (t >> 6) ? sums[1][w] : 0);
@@ -77,15 +167,22 @@ __global__ __launch_bounds__(1024) void list_kernel(const uint8_t* mask, TokenRo
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (bits >> i & 1) *to++ = at + i;
-    if (t == 0 && part + LIST_KEYS >= n) count[b] = all;
+    if (!COUNTED && t == 0 && part + LIST_KEYS >= n) count[b] = all;
 }
 
 namespace {
 
-// What a call needs of its workspace: the splits' sums, the lists, their lengths.
+// Parts of a sequence up to which each workgroup of a list counts for itself (one query over a sequence of 64 parts,
+// counting itself 12.9 us, from counts 13.0; 128 parts 16.6 and 13.8; four sequences of 64 parts 13.6 and 15.1, of 128
+// 24.7 and 16.5; the counting grows with the square of the keys: 2^28 of them 1144 ms, from
+// counts 0.6).
+constexpr int COUNT_PARTS = 64;
+
+// What a call needs of its workspace: the splits' sums, the lists, their lengths, their parts' counts.
 struct CrossPlan {
     AttendCut cut;
     int queries, keys;     // rows that the sequences can have
+    int64_t slots;         // of parts, where they are counted first
     size_t list, all;
 };
 
@@ -115,7 +212,8 @@ bool cross_plan(const sscater_cross_spec* s, bool masked, CrossPlan* p) {
     p->keys = (int)std::min((int64_t)s->keys, (int64_t)s->max_k * s->batch);
     p->list = p->cut.splits > 1 ? (size_t)p->cut.splits * p->queries * s->q_heads * (s->head_dim + 2) * 4 : 0;
     p->list = (p->list + 15) / 16 * 16;
-    p->all = p->list + (masked && p->keys > 0 ? ((size_t)p->keys + s->batch) * 4 : 0);
+    p->slots = s->max_k > COUNT_PARTS * LIST_KEYS ? (int64_t)p->keys / LIST_KEYS + s->batch : 0;
+    p->all = p->list + (masked && p->keys > 0 ? ((size_t)p->keys + s->batch + p->slots) * 4 : 0);
     return true;
 }
 
@@ -198,11 +296,20 @@ int sscater_cross_attend(const sscater_cross_spec* spec, const void* q, const vo
         TokenRows keys;
         keys.tokens = p.keys; keys.max_new = spec->max_k; keys.batch = spec->batch; keys.start = spec->k_start;
         keys.past = nullptr;
-        const int64_t parts = std::max(1, (spec->max_k + LIST_KEYS - 1) / LIST_KEYS), groups = parts * spec->batch;
+        const hipStream_t on = (hipStream_t)stream;
+        int32_t *const count = list + p.keys, *const counts = count + spec->batch;
+        if (p.slots) {
+            for (int64_t id = 0; id < p.slots; id += LAUNCH_GROUPS)
+                count_kernel<<<dim3((unsigned)std::min(LAUNCH_GROUPS, p.slots - id)), dim3(256), 0, on>>>(mask, keys, counts, id);
+            before_kernel<<<dim3((unsigned)((spec->batch + 3) / 4)), dim3(256), 0, on>>>(keys, counts, count);
+        }
+        const int64_t parts = std::max(1, (spec->max_k + LIST_KEYS - 1) / LIST_KEYS), groups = p.slots ? p.slots : parts * spec->batch;
         constexpr int64_t LAUNCH = LAUNCH_GROUPS / 4;  // workgroups of 1024 threads
-        for (int64_t id = 0; id < groups; id += LAUNCH)
-            list_kernel<<<dim3((unsigned)std::min(LAUNCH, groups - id)), dim3(1024), 0, (hipStream_t)stream>>>(
-                mask, keys, list, list + p.keys, (int)parts, id);
+        for (int64_t id = 0; id < groups; id += LAUNCH) {
+            const dim3 grid((unsigned)std::min(LAUNCH, groups - id)), block(1024);
+            if (p.slots) list_kernel<true><<<grid, block, 0, on>>>(mask, keys, list, count, counts, 0, id);
+            else list_kernel<false><<<grid, block, 0, on>>>(mask, keys, list, count, nullptr, (int)parts, id);
+        }
     }
     const bool one = spec->rounded != 0;
     if (listed) launch_cross<Keys::LISTED>(a, p.cut, f32, one, spec->head_dim, (hipStream_t)stream);
