@@ -282,7 +282,8 @@ __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
             for (int e = 0; e < E; ++e) {
                 const float kv = __uint_as_float(F32 ? ku[e & 3] : e & 1 ? ku[e / 2] & 0xFFFF0000u : ku[e / 2] << 16);
                 const float qv = __uint_as_float(F32 ? qu[e & 3] : e & 1 ? qu[e / 2] & 0xFFFF0000u : qu[e / 2] << 16);
-                odd |= !finite(kv);
+                // (an infinite query has the state's sign, which a sum over the stretch's tokens would lose)
+                odd |= !finite(kv) || (!a.unit && fabsf(qv) == INFINITY);
                 kk = fmaf(kv, kv, kk);
                 qq = fmaf(qv, qv, qq);
             }
