@@ -24,9 +24,9 @@
 // part, an error as large as the output's rounding (a window of 33480 tokens 1920
 // us, in two parts 2680; 48 rows over 16384 keys 30.9 and 33.1); of another set of
 // tokens two, and one where the caller asks for it (900 queries of four maps of
-// 53568 cells, 16 heads of 64 on 4: 1440 us, in one part 1010; 8 heads of 32, a
+// 53568 cells, 16 heads of 64 on 4: 1370 us, in one part 980; 8 heads of 32, a
 // quarter of the cells visible: 161 and 117; 500 queries over two times 20000 keys,
-// 8 heads of 128 on 4: 132 and 100).  The sum is of the unrounded probabilities.
+// 8 heads of 128 on 4: 126 and 96).  The sum is of the unrounded probabilities.
 //
 // WM of the four wavefronts share keys and take different rows, the other
 // 4 / WM groups take other tiles of keys and are joined at the end.  Where the
@@ -69,6 +69,16 @@ struct AttendArgs {
     const int32_t* list;
     const int32_t* count;
 };
+
+// Two probabilities in two bf16 parts each: the first 8 bits, and what is left rounded to 8, off by 2^-16 of them.  The
+// second part of one that is not zero is not either, nor negative (a 2^-23rd of it is added): an infinite value times both
+// is that infinity, not NaN.
+__device__ __forceinline__ void two_parts(float x, float y, uint32_t& first, uint32_t& second) {
+    constexpr float MORE = 1.f + 0x1p-23f;
+    const uint32_t ux = __float_as_uint(x), uy = __float_as_uint(y);
+    first = __builtin_amdgcn_perm(uy, ux, 0x07060302u);
+    second = bf16_pair(fmaf(x, MORE, -__uint_as_float(ux & 0xFFFF0000u)), fmaf(y, MORE, -__uint_as_float(uy & 0xFFFF0000u)));
+}
 
 template <bool F32, int D, int WM>
 struct AttendShape {
@@ -530,11 +540,10 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
                     uint32_t w[3];
                     if constexpr (C::PL)
                         cut_pair(__float_as_uint(s[e >> 4][(e & 15) - 1]), __float_as_uint(x), w[0], w[1], w[2]);
+                    else if constexpr (PP == 2)
+                        two_parts(s[e >> 4][(e & 15) - 1], x, w[0], w[1]);
                     else
                         w[0] = bf16_pair(s[e >> 4][(e & 15) - 1], x);
-                    if constexpr (PP == 2)
-                        w[1] = bf16_pair(s[e >> 4][(e & 15) - 1] - __uint_as_float(w[0] << 16),
-                                         x - __uint_as_float(w[0] & 0xFFFF0000u));
 #pragma unroll
                     for (int p = 0; p < PP; ++p) {
                         uint4& f = pf[e >> 3][p];
@@ -609,16 +618,6 @@ __global__ __launch_bounds__(256, (AttendShape<F32, D, WM>::WGS)) void attend_ke
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < 4; ++g) again |= ml[g][0][0] != 0.f;
-    }
-    if constexpr (PP == 2) {
-        // A probability's second part may be zero or negative, and an infinite value times that makes a sum NaN: such sums
-        // are formed again.
-        float any = 0.f;
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) any += o[t][e];
-        again |= __ballot(any != any) != 0;
     }
     if (again) {
         // Keys one by one, each only for the rows that see it: the wavefront's
