@@ -229,6 +229,7 @@ __device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0
 __device__ __forceinline__ bool beyond(float v, int e) { return (__float_as_uint(v) & 0x7F800000u) >= (uint32_t)(127 + e) << 23; }
 // T and X below these make 64 sums that are finite.
 constexpr int T_LIMIT = 20, X_LIMIT = 100;
+constexpr int MAX_FLAGS = 32;                          // of a part: see state_kernel
 
 // A workgroup a stretch and head: scores of keys and queries (bf16 in bf16 instructions: exact products), T by
 // substitution in the diagonal tiles and products below them.  (12312 stretches of fp32 heads of 64: 205 us for 265 MB
@@ -469,16 +470,25 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     if (seg > 0 ? c0 == all : unit) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int w = wave & 3, wq = 3 - w, col = (block - (unit ? DV / 16 : 0)) * 16 + r;
-    // a part's M, as first operands, and B, as results
-    constexpr int PART = DK * DK + DK * DV;
+    // a part's M, as first operands, B, as results, and whether M has large values, infinities or NaN (of the wavefronts that
+    // formed it)
+    constexpr int PART_FLAGS = DK * DK + DK * DV, FLAGS = DK / 16 * 4, PART = PART_FLAGS + MAX_FLAGS;
     float* const part0 = parts + which * a.parts * PART;
+    // A product with such an M may be infinite or NaN where the tokens one after the other are not (a large key before which
+    // the memory is empty): the stretches of all parts before are gone through here, too.
+    bool whole = false;
+    if constexpr (OUT) {
+        for (int i = lane; i < (seg - 1) * FLAGS; i += 64) whole |= part0[(1 + i / FLAGS) * PART + PART_FLAGS + i % FLAGS] != 0.f;
+        whole = __ballot(whole) != 0;
+    }
+    const int cb = whole ? 0 : c0, joins = whole ? 1 : seg;
     auto b_of = [&](int j, int tile) __attribute__((always_inline)) {
         return (f4v*)(part0 + j * PART + DK * DK + ((int64_t)tile * (DV / 16) + block) * 256 + lane * 4);
     };
     // of the stretch whose operands are loaded next, moved on from one to the next: a stretch's worth of scalar
     // multiplications is time on every wavefront's way
-    const int64_t row0 = first + (int64_t)c0 * CHUNK, step_m = (int64_t)a.heads * MATS;
-    const float* mx = mats + ((int64_t)(slot_of(first, b) + c0) * a.heads + h) * MATS;
+    const int64_t row0 = first + (int64_t)cb * CHUNK, step_m = (int64_t)a.heads * MATS;
+    const float* mx = mats + ((int64_t)(slot_of(first, b) + cb) * a.heads + h) * MATS;
     const float *mu = mx, *ms = mx;
     const uint32_t ldk = (uint32_t)a.ldk * S, ldq = (uint32_t)a.ldq * S, ldv = (uint32_t)a.ldv * S;
     auto tokens = [&](int c) __attribute__((always_inline)) { return min(CHUNK, n - c * CHUNK); };
@@ -613,23 +623,23 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
 #pragma unroll
             for (int t = 0; t < NT; ++t) k[t].load(from + off + 16 * t * S, 0);
         };
-        if (chunks > c0) {
-            load_k(c0);
-            load_q(c0);
+        if (chunks > cb) {
+            load_k(cb);
+            load_q(cb);
             load_p();
-            keep_keys(k, w, kbuf + (c0 & 1) * KEYS);
-            if (c0 + 1 < chunks) from += step_k;
-            load_k(min(c0 + 1, chunks - 1));
+            keep_keys(k, w, kbuf + (cb & 1) * KEYS);
+            if (cb + 1 < chunks) from += step_k;
+            load_k(min(cb + 1, chunks - 1));
         }
         const int64_t out_row = (int64_t)a.heads * DV;
         char* to = (char*)a.out + ((row0 + 16 * wq + 4 * g) * out_row + h * DV + col) * S;
         lds_barrier();
-        for (int j = 1; j < seg; ++j) {
+        for (int j = 1; j < joins; ++j) {
             lds_barrier();
             lds_barrier();
         }
 #pragma unroll 1
-        for (int c = c0; c < chunks; ++c) {
+        for (int c = cb; c < chunks; ++c) {
             const int m = tokens(c), next = min(c + 1, chunks - 1);
             // beside the chain's first product
             const Rows queries = operands(q);
@@ -658,7 +668,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
             for (int e = 0; e < 4; ++e) {
                 const float v = o[0][e] + o[1][e];
                 char* const at = to + e * out_row * S;
-                if (16 * wq + 4 * g + e < m && !(columns >> r & 1)) {
+                if (16 * wq + 4 * g + e < m && !(columns >> r & 1) && c >= c0) {
                     if constexpr (F32) *(float*)at = v;
                     else *(uint16_t*)at = (uint16_t)bf16_pair(v, v);
                 }
@@ -684,7 +694,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
     for (int o = 0; o < OWN; ++o) {
         if (OUT && a.parts > 1) {
             // the state put aside, or the first part's end
-            s[o] = *b_of(seg == 0 ? a.parts - 1 : 0, tile(o));
+            s[o] = *b_of(seg == 0 || whole ? a.parts - 1 : 0, tile(o));
         } else if (seg == 0) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[o][e] = a.from[state_at(o, e)];
@@ -789,20 +799,20 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
                 o = fmaf(z[j], q[j], o);
             }
             o = sum(o, 1) * fq;
-            if (OUT && p == 0 && (columns >> r & 1)) put(t, o);
+            if (OUT && p == 0 && (columns >> r & 1) && c >= c0) put(t, o);
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) *place(zbuf, i) = z[i];
     };
-    if (chunks > c0) {
-        load_x(c0);
+    if (chunks > cb) {
+        load_x(cb);
         load_u();
         load_s();
     }
     lds_barrier();
     if constexpr (OUT) {
 #pragma unroll 1
-        for (int j = 1; j < seg; ++j) {
+        for (int j = 1; j < joins; ++j) {
             f4v y[OWN];
 #pragma unroll
             for (int o = 0; o < OWN; ++o) {
@@ -822,7 +832,7 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         }
     }
 #pragma unroll 1
-    for (int c = c0; c < chunks; ++c) {
+    for (int c = cb; c < chunks; ++c) {
         const int m = tokens(c), next = min(c + 1, chunks - 1);
         char* const kb = kbuf + (OUT ? (c & 1) * KEYS : 0);
         f4v x;
@@ -912,6 +922,15 @@ __global__ __launch_bounds__(OUT ? 512 : 256) void state_kernel(DeltaArgs a, con
         load_s();
         lds_barrier();
     }
+    if (!OUT && unit) {
+        bool large = false;
+#pragma unroll
+        for (int o = 0; o < OWN; ++o)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) large |= beyond(s[o][e], T_LIMIT);
+        large = __ballot(large) != 0;
+        if (lane == 0) part0[seg * PART + PART_FLAGS + col / 16 * 4 + w] = large ? 1.f : 0.f;
+    }
     if (!own) return;
 #pragma unroll
     for (int o = 0; o < OWN; ++o) {
@@ -980,7 +999,7 @@ DeltaPlan delta_plan(const sscater_delta_memory* m, const sscater_token_rows* r)
 }
 
 size_t delta_bytes(const DeltaPlan& p, const sscater_delta_memory* m) {
-    const size_t part = (size_t)m->key_dim * (m->key_dim + m->value_dim);
+    const size_t part = (size_t)m->key_dim * (m->key_dim + m->value_dim) + MAX_FLAGS;
     return 4 * m->heads * (p.slots * (size_t)MATS + (p.parts > 1 ? (size_t)m->batch * p.parts * part : 0));
 }
 
