@@ -525,8 +525,8 @@ typedef struct {
  * i's sequence, query head h reading key and value head h / (q_heads / kv_heads);
  * zeros where no key is visible.  mask: device bytes [keys], zero where a key is
  * not visible (its k and v are not read), or NULL; out: device [queries][q_heads]
- * [head_dim], on a 16-byte boundary.  Queries behind the last sequence's are left
- * as they were.  Scores, maxima and sums are fp32; for their product with bf16 values
+ * [head_dim], on a 16-byte boundary, overlapping no operand.  Queries behind the last
+ * sequence's are left as they were.  Scores, maxima and sums are fp32; for their product with bf16 values
  * probabilities are held in two bf16 parts (16 bits), or, with rounded = 1, rounded to
  * bf16 where a sequence may bring more than 32 rows (max_q * q_heads / kv_heads): an
  * error as large as the output's rounding, in some seven tenths of the time.
@@ -550,7 +550,8 @@ typedef struct {
 } sscater_delta_memory;
 
 /*   unit = 1: queries and keys are taken to unit length first, x / sqrt(sum x^2 +
- *   eps), the squares summed in fp32 as in the norms; *_stride: elements from token to token, at most 2^24 for q, k and v. */
+ *   eps), the squares summed in fp32 as in the norms; *_stride: elements from token to
+ *   token, at most 2^24 for q, k and v. */
 typedef struct {
     int32_t unit;
     float eps, scale;
@@ -570,7 +571,9 @@ typedef struct {
  * the state from bf16 planes that hold its 24 bits, of values from 2^-110 on), tokens
  * one by one or in stretches of 64, which differ in their last bits.  No token
  * depends on a later one, whatever that holds.  Rows behind the last stream's are left as
- * they were.  The workspace is as for attention. */
+ * they were.  out and memory->state overlap no operand (initial may be the state itself).
+ * The workspace is as for attention; in stretches it has 21.6 KB for each of them and head
+ * (2^20 tokens of 32 heads: 11.3 GB). */
 int sscater_delta_workspace(const sscater_delta_spec* spec, const sscater_delta_memory* memory,
                             const sscater_token_rows* rows, size_t* bytes);
 int sscater_delta_update(const sscater_delta_spec* spec, const sscater_delta_memory* memory,

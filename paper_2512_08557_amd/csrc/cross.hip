@@ -10,7 +10,8 @@
 // Bound by the softmax's vector instructions and the products with the values, twice as
 // many as with the keys (3600 queries, a quarter of four times 53568 cells visible, 8
 // bf16 heads of 32: 161 us; all cells, 16 heads of 64 on 4: 1370 us, 577 TFLOP/s of the
-// formula's; with probabilities rounded to bf16 117 and 980).
+// formula's; with probabilities rounded to bf16 117 and 980).  Matrix cores are busy 21
+// and 37 % of the time.
 #include "attend_kernel.h"
 
 #include <algorithm>

@@ -232,7 +232,7 @@ constexpr int T_LIMIT = 20, X_LIMIT = 100;
 constexpr int MAX_FLAGS = 32;                          // of a part: see state_kernel
 
 // A workgroup a stretch and head: scores of keys and queries (bf16 in bf16 instructions: exact products), T by
-// substitution in the diagonal tiles and products below them.  (12312 stretches of fp32 heads of 64: 205 us for 265 MB
+// substitution in the diagonal tiles and products below them.  (12312 stretches of fp32 heads of 64: 215 us for 265 MB
 // written and twice that read; matrix cores 30 % busy.)
 template <bool F32, int DK>
 __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
@@ -435,8 +435,8 @@ __global__ __launch_bounds__(256) void chunk_kernel(DeltaArgs a, float* mats) {
 // the product of the parts before theirs.
 //
 // Bound by the way through a stretch: three products and meetings after one another, 2.1 us (523 stretches, four streams,
-// 8 fp32 heads of 64 x 128: 1080 us with 256 workgroups, with fp32 products throughout 1180; 3348 tokens of 8 bf16 heads
-// of 64 x 64 in eight parts: 19 and 22, 23 and 26).  Keys and queries are cut while the chain is at its first product; in
+// 8 fp32 heads of 64 x 128: 1120 us with 256 workgroups, with fp32 products throughout a tenth more; 3348 tokens of 8 bf16
+// heads of 64 x 64 in eight parts: 20 and 22, 23 and 26).  Keys and queries are cut while the chain is at its first product; in
 // the second's time, cutting was 70 us more.  Matrices that come from memory later than a stretch after their loads are 70
 // us of it; touching them three stretches ahead, by the outputs' wavefronts or by a ninth, gave none of that back.
 template <bool F32, int DK, int DV, bool OUT>
@@ -974,7 +974,11 @@ void launch_chunks(DeltaArgs a, int64_t slots, float* mats, hipStream_t s) {
 // states 4 for each round over the card, chunk_kernel 1 for 150 heads' stretches, 80 of fp32; the further launches 5 each.
 // (Heads of 64 x 64 in bf16, one by one and in stretches: 8 heads, 8 tokens 10.2 and 13.2, 16 tokens 16.0 and 13.2, 64
 // tokens 49 and 14; 128 heads, 16 tokens 16.3 and 18.3, 32 tokens 27.6 and 18.8; 8000 heads, 64 tokens 462 and 715, 192
-// tokens 1329 and 1288; 4000 heads in fp32, 192 tokens 651 and 848; 2400 heads of 32 x 32, 64 tokens 76 and 118.)
+// tokens 1329 and 1288; 4000 heads in fp32, 192 tokens 651 and 848; 2400 heads of 32 x 32, 64 tokens 76 and 118.  Of 128 x
+// 128 in bf16: 8 heads, 8 tokens 14.1 and 13.8, 16 tokens 22.7 and 14.1; 128 heads, 16 tokens 24.1 and 30.5, 32 tokens 40.6
+// and 31.2; 2000 heads, 64 tokens 460 and 475, 192 tokens 1361 and 843; in fp32 8 heads, 8 tokens 13.5 and 17.1, 16 tokens
+// 20.9 and 17.6; 128 heads, 32 tokens 37.0 and 37.7, 64 tokens 66.9 and 42.7; 2000 heads, 192 tokens 1250 and 1063.  The
+// constants are the same for them, which is wrong only for thousands of heads and tokens enough: there they go one by one.)
 DeltaPlan delta_plan(const sscater_delta_memory* m, const sscater_token_rows* r) {
     DeltaPlan p = {0, 1, 0};
     const bool f32 = m->dtype == SSCATER_F32;

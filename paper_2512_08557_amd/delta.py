@@ -84,7 +84,9 @@ class DeltaMemory:
         and bias (float32 [heads]): alpha = exp(-rate softplus(a + bias)) and beta =
         sigmoid(b); without them alpha = exp(a), a <= 0, and beta = b.  scale: 1 /
         sqrt(key_dim) unless given.  initial: states to begin from instead of the
-        memory's (which are written all the same)."""
+        memory's (which are written all the same).  out: the result's shape, contiguous;
+        it and the state overlap no operand (initial may be the state itself).  Long
+        streams take a workspace of 21.6 KB for every 64 tokens and head."""
         index = self.index
         if self._state.requires_grad:
             T._want_gradient()
