@@ -526,10 +526,11 @@ typedef struct {
  * zeros where no key is visible.  mask: device bytes [keys], zero where a key is
  * not visible (its k and v are not read), or NULL; out: device [queries][q_heads]
  * [head_dim], on a 16-byte boundary, overlapping no operand.  Queries behind the last
- * sequence's are left as they were.  Scores, maxima and sums are fp32; for their product with bf16 values
- * probabilities are held in two bf16 parts (16 bits), or, with rounded = 1, rounded to
- * bf16 where a sequence may bring more than 32 rows (max_q * q_heads / kv_heads): an
- * error as large as the output's rounding, in some seven tenths of the time.
+ * sequence's are left as they were.  Scores, maxima and sums are fp32; for their
+ * product with bf16 values probabilities are held in two bf16 parts (16 bits), or, with
+ * rounded = 1, rounded to bf16 where a sequence may bring more than 32 rows (max_q *
+ * q_heads / kv_heads): an error as large as the output's rounding, in some seven tenths
+ * of the time.
  * workspace: as there, sscater_cross_workspace() bytes (masked: also without
  * splits).  `masked`: whether there will be a mask. */
 int sscater_cross_workspace(const sscater_cross_spec* spec, int32_t masked, size_t* bytes);

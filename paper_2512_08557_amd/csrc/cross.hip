@@ -178,6 +178,11 @@ namespace {
 // 24.7 and 16.5; the counting grows with the square of the keys: 2^28 of them 1144 ms, from
 // counts 0.6).
 constexpr int COUNT_PARTS = 64;
+// Where the longest sequence is not known, or much longer than the others, most workgroups have no part; so many, and for
+// each that may have one so many more, are left to find that out (100 sequences with 209000 keys in all, 5100 workgroups
+// for 150: counting itself 22.3 us, from counts 26.8; 300, 15900 for 350: 35.4 and 23.8; 20000, 940000 for 20046: 1552 and
+// 317; 100000 with 150000 keys 6190 and 1640).
+constexpr int64_t COUNT_SPARE = 8192, COUNT_SPARE_EACH = 8;
 
 // What a call needs of its workspace: the splits' sums, the lists, their lengths, their parts' counts.
 struct CrossPlan {
@@ -213,7 +218,9 @@ bool cross_plan(const sscater_cross_spec* s, bool masked, CrossPlan* p) {
     p->keys = (int)std::min((int64_t)s->keys, (int64_t)s->max_k * s->batch);
     p->list = p->cut.splits > 1 ? (size_t)p->cut.splits * p->queries * s->q_heads * (s->head_dim + 2) * 4 : 0;
     p->list = (p->list + 15) / 16 * 16;
-    p->slots = s->max_k > COUNT_PARTS * LIST_KEYS ? (int64_t)p->keys / LIST_KEYS + s->batch : 0;
+    p->slots = (int64_t)p->keys / LIST_KEYS + s->batch;
+    const int64_t parts = ((int64_t)s->max_k + LIST_KEYS - 1) / LIST_KEYS;
+    if (parts <= COUNT_PARTS && parts * s->batch <= COUNT_SPARE + COUNT_SPARE_EACH * p->slots) p->slots = 0;
     p->all = p->list + (masked && p->keys > 0 ? ((size_t)p->keys + s->batch + p->slots) * 4 : 0);
     return true;
 }

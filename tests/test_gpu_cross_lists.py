@@ -81,19 +81,20 @@ def test_sequences_of_different_lengths(queries):
             a, c = a + n, c + m
 
 
-def test_many_sequences_whose_longest_is_not_known():
-    """The most of one sequence is taken to be all: 20000 of up to 40 keys."""
+@pytest.mark.parametrize("batch,most", [(20000, 40), (3000, 120), (100000, 3), (150, 1400), (40, 9000)])
+def test_many_sequences_whose_longest_is_not_known(batch, most):
+    """The most of one sequence is taken to be all; counted first and not."""
+    note(f"[gpu-test] {batch} masked sequences of less than {most} keys")
     rng = np.random.default_rng(5)
-    nk = rng.integers(0, 40, 20000)
+    nk = rng.integers(0, most, batch)
     total = int(nk.sum())
-    q, k, v = normal(rng, (20000, 1, 32)), normal(rng, (total, 1, 32)), normal(rng, (total, 1, 32))
+    q, k, v = normal(rng, (batch, 1, 32)), normal(rng, (total, 1, 32)), normal(rng, (total, 1, 32))
     seen = torch.from_numpy(rng.random(total) < 0.3).cuda()
-    starts = [torch.from_numpy(np.concatenate([[0], np.cumsum(n)]).astype(np.int32)).cuda() for n in (np.ones(20000, np.int64), nk)]
-    assert total > 262144
+    starts = [torch.from_numpy(np.concatenate([[0], np.cumsum(n)]).astype(np.int32)).cuda() for n in (np.ones(batch, np.int64), nk)]
     out = ssc.cross_attend(q, k, v, seen, *starts, max_q=1)
-    want = ssc.cross_attend(q, k, v, seen, *starts, max_q=1, max_k=39)
+    want = ssc.cross_attend(q, k, v, seen, *starts, max_q=1, max_k=most - 1)
     at = np.concatenate([[0], np.cumsum(nk)])
-    for b in list(range(0, 20000, 2500)) + [19999]:
+    for b in list(range(0, batch, batch // 8)) + [batch - 1]:
         s = slice(int(at[b]), int(at[b + 1]))
         check(out[b:b + 1], q[b:b + 1], k[s], v[s], seen[s], f"sequence {b}")
     none = torch.tensor([not bool(x) for x in np.add.reduceat(np.append(seen.cpu().numpy(), False), at[:-1]) * (nk > 0)])
